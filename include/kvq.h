@@ -285,6 +285,65 @@ kvq_status kvq_decode_step_varlen(const kvq_layout* layout, const kvq_cache* cac
                                   int32_t q_heads, float softmax_scale, void* out, kvq_dtype out_dtype, void* workspace,
                                   size_t workspace_bytes, void* stream);
 
+/* ---- Several tokens per sequence: prompts in chunks, verification of drafted tokens, sliding windows -----------------------
+ * The three calls below take caches with token-wise keys and without a residual buffer (KVQ_ERR_UNSUPPORTED otherwise), of every
+ * width, group size, rotation and page size, and 1 to 8 query heads per KV head. */
+
+/* Rotation of positions: the angles' cosines and sines as the caller's model defines them. */
+typedef struct {
+  const float* cos;      /* device, [rows][rotary_dim / 2] contiguous binary32, 16-byte aligned: row p belongs to position p */
+  const float* sin;
+  int32_t rows;          /* positions that the tables hold */
+  int32_t rotary_dim;    /* channels [0, rotary_dim) of a row are rotated (a multiple of 16, 16 .. head_dim), the others kept */
+  int32_t interleaved;   /* 0: channel i < rotary_dim/2 pairs with i + rotary_dim/2;  1: channel 2i pairs with 2i + 1 */
+} kvq_rope;
+
+/* Append tokens to every sequence at its own position, with the rotation of their positions applied on the way:
+ *   token i < n_tokens[b] of sequence b goes to position p = pos[b] + i; the pairs (x1, x2) of its query and key rows become
+ *   (x1 cos - x2 sin, x2 cos + x1 sin), cos and sin of row p, each operation rounded once in binary32;
+ *   rotated queries are rounded once to in_dtype and written to q_out; rotated keys go to the quantizer in binary32 (bits_k == 16:
+ *   rounded once to raw_dtype), after the rotation of rotate_k where the layout has it; values as in kvq_quantize_append.
+ * The stored bytes are those of kvq_quantize_append on keys rotated that way, wherever those are exact in in_dtype.
+ *   q              [B][n_new][q_heads][D] of in_dtype, element strides given, D contiguous, 16-byte aligned rows; or NULL (then q_heads = 0
+ *                  and q_out = NULL): nothing but the append.
+ *   q_out          [B][n_new][q_heads][D] contiguous of in_dtype; may be q itself where q is contiguous.
+ *   k_new, v_new   [B][H_kv][n_new][D] of in_dtype, element strides given as in kvq_quantize_append.
+ *   pos            device, int32[B].  n_tokens: device, int32[B], clamped to [0, n_new]; NULL: n_new each.
+ * A token whose position is negative, or not below both max_seq and rope->rows, is left out: nothing of it is stored, and its row of q_out
+ * stays as it is, as do the rows of tokens from n_tokens[b] on.  n_new == 0 is a no-op. */
+kvq_status kvq_rope_append(const kvq_layout* layout, const kvq_cache* cache, const void* q, int64_t q_stride_b, int64_t q_stride_t,
+                           int64_t q_stride_h, int32_t q_heads, void* q_out, const void* k_new, const void* v_new,
+                           kvq_dtype in_dtype, int64_t stride_b, int64_t stride_h, int64_t stride_t, const int32_t* pos,
+                           const int32_t* n_tokens, int32_t n_new, const kvq_rope* rope, void* stream);
+
+/* Causal attention of the last q_lens[b] tokens of every sequence over its cached tokens, themselves included (append them first):
+ * query token i of sequence b sits at position p = seq_lens[b] - q_lens[b] + i and sees the cached tokens t <= p with
+ *   window == 0, or t > p - window, or t < sinks:
+ * all of them, or the newest `window` (its own among them) and the first `sinks`.  A query with p < 0 sees nothing; its output is 0.
+ *   q              [B][n_q][q_heads][D], KVQ_F16 or KVQ_BF16, element strides given, D contiguous, 16-byte aligned rows (bfloat16 is
+ *                  converted to binary16: values beyond its range are not supported, those below 2^-14 lose bits).
+ *   q_lens         device, int32[B], clamped to [0, n_q]; NULL: n_q each.  Rows of `out` from q_lens[b] on stay as they are.
+ *   seq_lens       device, int32[B], clamped to [0, max_seq_len]; NULL: max_seq_len each.
+ *   out            [B][n_q][q_heads][D] contiguous, KVQ_F32, KVQ_F16 or KVQ_BF16 (rounded once).
+ *   workspace      kvq_chunk_workspace_bytes(layout, q_heads, n_q, max_seq_len, window, sinks) bytes, 16-byte aligned; with fewer (or
+ *                  NULL) the tokens are cut into fewer parts, which is slower, and rounds differently.  What it holds before a call does
+ *                  not matter; calls that overlap in time need one each.
+ * n_q == 0 is a no-op.  Values that a cache holds in places no query sees (behind a sequence's end, in unused pages) are never used. */
+kvq_status kvq_chunk_workspace_bytes(const kvq_layout* layout, int32_t q_heads, int32_t n_q, int32_t max_seq_len, int32_t window,
+                                     int32_t sinks, size_t* bytes_out);
+kvq_status kvq_chunk_attention(const kvq_layout* layout, const kvq_cache* cache, const void* q, kvq_dtype q_dtype, int32_t q_heads,
+                               int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int32_t n_q, const int32_t* q_lens,
+                               const int32_t* seq_lens, int32_t max_seq_len, int32_t window, int32_t sinks, float softmax_scale,
+                               void* out, kvq_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same for one query token per sequence (its newest, position seq_lens[b] - 1): decoding with a sliding window and sinks.
+ *   q    [B][q_heads][D] contiguous;  out  [B][q_heads][D] contiguous;  everything else as in kvq_chunk_attention. */
+kvq_status kvq_window_workspace_bytes(const kvq_layout* layout, int32_t q_heads, int32_t max_seq_len, int32_t window, int32_t sinks,
+                                      size_t* bytes_out);
+kvq_status kvq_window_attention(const kvq_layout* layout, const kvq_cache* cache, const void* q, kvq_dtype q_dtype, int32_t q_heads,
+                                const int32_t* seq_lens, int32_t max_seq_len, int32_t window, int32_t sinks, float softmax_scale,
+                                void* out, kvq_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Reconstruct tokens [t0, t1) as x^ = code * scale + zero (App. B "Dequantization"):
  *   k_out, v_out  [B][H_kv][t1-t0][D] contiguous of out_dtype; either may be NULL to skip it.
  * KVQ_F32 output is exactly the binary32 value; 16-bit outputs round it once. */

@@ -41,6 +41,8 @@ UNITS = [("kvq_api.hip", "kvq_api.o", []),
          ("kvq_seq_append.hip", "kvq_seq_append.o", ["-ffp-contract=off"]),      # (value patterns one at a time, and the launchers)
          ("kvq_seq_append.hip", "kvq_seq_append_quads.o", ["-ffp-contract=off", "-DKVQ_SA_QUADS"]),      # (four at a time)
          ("kvq_readback.hip", "kvq_readback.o", ["-ffp-contract=off"]),
+         ("kvq_rope.hip", "kvq_rope.o", ["-ffp-contract=off"]),
+         ("kvq_chunk.hip", "kvq_chunk.o", ["-Rpass-analysis=kernel-resource-usage"]),
          ("kvq_decode.hip", "kvq_decode.o", [])]
 UNITS += [("kvq_decode.hip", f"kvq_decode_k{bk}v{bv}.o",
            [f"-DKVQ_INST_BK={bk}", f"-DKVQ_INST_BV={bv}", "-Rpass-analysis=kernel-resource-usage"]) for bk, bv in DECODE_PAIRS]

@@ -314,6 +314,131 @@ kvq_status kvq_decode_step_varlen(const kvq_layout* layout, const kvq_cache* cac
                        workspace_bytes, &app, stream, pos, 1);
 }
 
+// ---- several tokens per sequence ------------------------------------------------------------------------------------------
+namespace {
+// The caches that the calls below take: token-wise keys without a residual buffer.
+kvq_status several_tokens_supported(const kvq_layout* L) {
+  return kvq::has_residual(*L) ? KVQ_ERR_UNSUPPORTED : KVQ_OK;
+}
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+kvq_status chunk_check(const kvq_layout* L, int32_t q_heads, int32_t n_q, int32_t max_seq_len, int32_t window, int32_t sinks) {
+  kvq_status st = check_layout(L);
+  if (st != KVQ_OK) return st;
+  if (q_heads <= 0 || q_heads % L->kv_heads || n_q < 0 || max_seq_len < 0 || window < 0 || sinks < 0) return KVQ_ERR_INVALID_ARG;
+  if (max_seq_len > L->max_seq) return KVQ_ERR_CAPACITY;
+  if (q_heads / L->kv_heads > 8) return KVQ_ERR_UNSUPPORTED;
+  if (n_q > (1 << 19)) return KVQ_ERR_UNSUPPORTED;             // (row tiles of a launch stay below 65536)
+  return several_tokens_supported(L);
+}
+
+kvq_status chunk_common(const kvq_layout* layout, const kvq_cache* cache, const void* q, kvq_dtype q_dtype, int32_t q_heads,
+                        int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int32_t n_q, const int32_t* q_lens,
+                        const int32_t* seq_lens, int32_t max_seq_len, int32_t window, int32_t sinks, float softmax_scale,
+                        void* out, kvq_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  kvq_status st = chunk_check(layout, q_heads, n_q, max_seq_len, window, sinks);
+  if (st != KVQ_OK) return st;
+  st = check_cache(layout, cache);
+  if (st != KVQ_OK) return st;
+  if (q_dtype != KVQ_F16 && q_dtype != KVQ_BF16) return KVQ_ERR_INVALID_ARG;
+  if (out_dtype != KVQ_F32 && out_dtype != KVQ_F16 && out_dtype != KVQ_BF16) return KVQ_ERR_INVALID_ARG;
+  if (!(softmax_scale > 0.0f) || softmax_scale > 3.0e38f) return KVQ_ERR_INVALID_ARG;   // positive and finite
+  if (!aligned4(q_lens) || !aligned4(seq_lens)) return KVQ_ERR_INVALID_ARG;
+  if (n_q == 0) return KVQ_OK;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return KVQ_ERR_INVALID_ARG;
+  if (q_stride_b % 8 || q_stride_t % 8 || q_stride_h % 8 || q_stride_h < layout->head_dim) return KVQ_ERR_INVALID_ARG;
+  if (workspace_bytes && workspace && !aligned16(workspace)) return KVQ_ERR_WORKSPACE;
+  kvq::ChunkArgs a{};
+  a.g = kvq::make_geom(*layout);
+  a.cache = *cache;
+  a.q = (const uint16_t*)q; a.q_bf16 = q_dtype == KVQ_BF16;
+  a.q_sb = q_stride_b; a.q_st = q_stride_t; a.q_sh = q_stride_h;
+  a.q_heads = q_heads; a.heads_per_kv = q_heads / layout->kv_heads; a.n_q = n_q;
+  a.q_lens = q_lens; a.seq_lens = seq_lens; a.seq_bound = max_seq_len;
+  a.window = window; a.sinks = sinks; a.softmax_scale = softmax_scale;
+  a.out = out; a.out_dtype = out_dtype;
+  a.ws = (float*)workspace;
+  a.splits = kvq::plan_chunk(a.g, a.heads_per_kv, n_q, max_seq_len, window, sinks);
+  const size_t record = kvq::chunk_record_bytes(layout->batch, n_q, q_heads, 2) / 2;
+  const size_t room = workspace ? workspace_bytes / record : 0;
+  if ((size_t)a.splits > room) a.splits = room < 2 ? 1 : (int32_t)room;
+  return kvq::launch_chunk_attention(a, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+}
+}  // namespace
+
+kvq_status kvq_chunk_workspace_bytes(const kvq_layout* layout, int32_t q_heads, int32_t n_q, int32_t max_seq_len, int32_t window,
+                                     int32_t sinks, size_t* bytes_out) {
+  kvq_status st = chunk_check(layout, q_heads, n_q, max_seq_len, window, sinks);
+  if (st != KVQ_OK) return st;
+  if (!bytes_out) return KVQ_ERR_INVALID_ARG;
+  const kvq::Geom g = kvq::make_geom(*layout);
+  *bytes_out = n_q == 0 ? 0 : kvq::chunk_record_bytes(layout->batch, n_q, q_heads,
+                                                      kvq::plan_chunk(g, q_heads / layout->kv_heads, n_q, max_seq_len, window, sinks));
+  return KVQ_OK;
+}
+
+kvq_status kvq_chunk_attention(const kvq_layout* layout, const kvq_cache* cache, const void* q, kvq_dtype q_dtype, int32_t q_heads,
+                               int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int32_t n_q, const int32_t* q_lens,
+                               const int32_t* seq_lens, int32_t max_seq_len, int32_t window, int32_t sinks, float softmax_scale,
+                               void* out, kvq_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  return chunk_common(layout, cache, q, q_dtype, q_heads, q_stride_b, q_stride_t, q_stride_h, n_q, q_lens, seq_lens, max_seq_len,
+                      window, sinks, softmax_scale, out, out_dtype, workspace, workspace_bytes, stream);
+}
+
+kvq_status kvq_window_workspace_bytes(const kvq_layout* layout, int32_t q_heads, int32_t max_seq_len, int32_t window, int32_t sinks,
+                                      size_t* bytes_out) {
+  return kvq_chunk_workspace_bytes(layout, q_heads, 1, max_seq_len, window, sinks, bytes_out);
+}
+
+kvq_status kvq_window_attention(const kvq_layout* layout, const kvq_cache* cache, const void* q, kvq_dtype q_dtype, int32_t q_heads,
+                                const int32_t* seq_lens, int32_t max_seq_len, int32_t window, int32_t sinks, float softmax_scale,
+                                void* out, kvq_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!layout) return KVQ_ERR_INVALID_ARG;
+  return chunk_common(layout, cache, q, q_dtype, q_heads, (int64_t)q_heads * layout->head_dim, layout->head_dim, layout->head_dim, 1,
+                      nullptr, seq_lens, max_seq_len, window, sinks, softmax_scale, out, out_dtype, workspace, workspace_bytes, stream);
+}
+
+kvq_status kvq_rope_append(const kvq_layout* layout, const kvq_cache* cache, const void* q, int64_t q_stride_b, int64_t q_stride_t,
+                           int64_t q_stride_h, int32_t q_heads, void* q_out, const void* k_new, const void* v_new,
+                           kvq_dtype in_dtype, int64_t stride_b, int64_t stride_h, int64_t stride_t, const int32_t* pos,
+                           const int32_t* n_tokens, int32_t n_new, const kvq_rope* rope, void* stream) {
+  kvq_status st = check_layout(layout);
+  if (st != KVQ_OK) return st;
+  st = check_cache(layout, cache);
+  if (st != KVQ_OK) return st;
+  if (!rope || !rope->cos || !rope->sin || !aligned16(rope->cos) || !aligned16(rope->sin) || rope->rows <= 0) return KVQ_ERR_INVALID_ARG;
+  if (rope->rotary_dim < 16 || rope->rotary_dim > layout->head_dim || rope->rotary_dim % 16) return KVQ_ERR_INVALID_ARG;
+  if (rope->interleaved != 0 && rope->interleaved != 1) return KVQ_ERR_INVALID_ARG;
+  if (n_new < 0 || !pos || !aligned4(pos) || !aligned4(n_tokens)) return KVQ_ERR_INVALID_ARG;
+  if (in_dtype != KVQ_F16 && in_dtype != KVQ_BF16) return KVQ_ERR_INVALID_ARG;
+  if ((layout->bits_k == 16 || layout->bits_v == 16) && (int)in_dtype != layout->raw_dtype) return KVQ_ERR_INVALID_ARG;
+  if (q) {
+    if (q_heads <= 0 || q_heads % layout->kv_heads || !q_out || !aligned16(q) || !aligned16(q_out)) return KVQ_ERR_INVALID_ARG;
+    if (q_stride_b % 8 || q_stride_t % 8 || q_stride_h % 8 || q_stride_h < layout->head_dim) return KVQ_ERR_INVALID_ARG;
+    if (q_heads / layout->kv_heads > 8) return KVQ_ERR_UNSUPPORTED;
+  } else if (q_heads != 0 || q_out) {
+    return KVQ_ERR_INVALID_ARG;
+  }
+  st = several_tokens_supported(layout);
+  if (st != KVQ_OK) return st;
+  if (n_new > layout->max_seq) return KVQ_ERR_CAPACITY;
+  if (n_new == 0) return KVQ_OK;
+  if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return KVQ_ERR_INVALID_ARG;
+  if (stride_b % 8 || stride_h % 8 || stride_t % 8 || stride_t < layout->head_dim) return KVQ_ERR_INVALID_ARG;
+  kvq::RopeArgs a{};
+  a.g = kvq::make_geom(*layout);
+  a.cache = *cache;
+  a.q = (const uint16_t*)q; a.q_out = (uint16_t*)q_out;
+  a.q_sb = q_stride_b; a.q_st = q_stride_t; a.q_sh = q_stride_h;
+  a.q_heads = q_heads; a.heads_per_kv = q_heads / layout->kv_heads;
+  a.k_new = (const uint16_t*)k_new; a.v_new = (const uint16_t*)v_new;
+  a.sb = stride_b; a.sh = stride_h; a.st = stride_t;
+  a.pos = pos; a.n_tokens = n_tokens; a.n_new = n_new;
+  a.capacity = layout->max_seq < rope->rows ? layout->max_seq : rope->rows;
+  a.cos_t = rope->cos; a.sin_t = rope->sin; a.rotary = rope->rotary_dim; a.interleaved = rope->interleaved;
+  return kvq::launch_rope_append(a, (int)in_dtype, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+}
+
 kvq_status kvq_dequantize(const kvq_layout* layout, const kvq_cache* cache, int32_t t0, int32_t t1, void* k_out,
                           void* v_out, kvq_dtype out_dtype, void* stream) {
   kvq_status st = check_layout(layout);

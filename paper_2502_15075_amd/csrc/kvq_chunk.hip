@@ -1,0 +1,529 @@
+// Attention of several query tokens per sequence over the packed cache (gfx950): chunks of a prompt, verification of
+// drafted tokens, with or without a sliding window and sinks.
+//
+//   S[t,i]  = sum_g sK[t,g] (sum_{d in g} q[i,d] cK[t,d]) + zK[t,g] (sum_{d in g} q[i,d])
+//   out[i]  = sum_t P[t,i] V^[t,:] / sum_t P[t,i],   P = 2^(kappa S - m),  kappa = softmax_scale log2 e
+//
+// The rows i of a kv head are its (query token, query head) pairs, token-major, so every row of a tile sees about the same tokens and
+// nothing is padded whatever the head ratio.  S is formed transposed (tokens x rows) by 32x32x16 matrix instructions: a lane then
+// owns one row of the softmax (its half of a tile's tokens), and its weights are in the place where the second product, channels x rows,
+// wants them.  Tokens reach the matrix rows with bits 3 and 4 of their number swapped, which makes the packed value blocks' order the
+// operand's order.
+//
+// A tile of 64 tokens is unpacked once per workgroup into LDS: keys as binary16 codes (0 .. 255: exact, so their products with the
+// query are too), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are rounded alike).  Key scales
+// are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the query's
+// group sums, each split into two binary16 parts.
+#include "kvq_internal.h"
+#include "kvq_quantizer.h"
+
+namespace kvq {
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNoMax = -1.0e30f;
+constexpr float kWeightBits = 10.0f;     // weights carry 2^10: small ones stay clear of binary16's subnormals
+constexpr float kMaxSlack = 4.0f;        // the running maximum is raised once it lags by more: weights stay below 2^14
+constexpr int kTileTokens = 64;
+constexpr int kRowsPerWave = 32, kWaves = 4, kTileRows = kRowsPerWave * kWaves;
+constexpr int kRec = kHeadDim + 4;       // floats of a partial record: 128 sums, maximum, weight sum
+
+__device__ __forceinline__ float16v mma32(u32x4 a, u32x4 b, float16v c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ half2v as_half2(uint32_t x) { return __builtin_bit_cast(half2v, x); }
+__device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ float other_half(float x) {           // lane ^ 32's value
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+// two whole numbers below 1024 in the halves of x -> the same as binary16
+__device__ __forceinline__ half2v whole_to_half2(uint32_t x) {
+  return as_half2(x | 0x64006400u) - half2v{(_Float16)1024.0f, (_Float16)1024.0f};
+}
+// Two patterns of the unquantized type -> binary16 (bfloat16: exact in binary16's normal range)
+__device__ __forceinline__ uint32_t raw_to_half2(uint32_t x, bool bf) {
+  if (!bf) return x;
+  half2v h;
+  h[0] = (_Float16)__uint_as_float(x << 16);
+  h[1] = (_Float16)__uint_as_float(x & 0xFFFF0000u);
+  return as_u32(h);
+}
+
+// Channel order inside a 32-channel chunk of an unpacked key row: with P = 16 / (field width), field pair (p, p + P) of dword w is
+// slots 2 (w P + p) and + 1.  The slot of channel x (0..31):
+__device__ __forceinline__ int key_slot(int x, int per) {
+  const int w = x / (2 * per), rem = x % (2 * per);
+  return 2 * (w * per + rem % per) + rem / per;
+}
+__device__ __forceinline__ int key_fields(int bits) { return bits == 3 ? 8 : bits == 6 ? 4 : 16 / bits; }
+
+// The codes of one 32-channel chunk (B dwords at p) as 16 binary16 pairs in slot order, four 16-byte pieces.
+template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* __restrict__ p, bool raw_bf, u32x4 (&out)[4]) {
+  constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
+  constexpr int P = 16 / LO;                       // pairs per dword
+  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
+  uint32_t w[B];
+  if constexpr (B % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < B / 4; ++i) *reinterpret_cast<u32x4*>(w + 4 * i) = reinterpret_cast<const u32x4*>(p)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < B; ++i) w[i] = p[i];
+  }
+#pragma unroll
+  for (int s = 0; s < 16; ++s) {
+    const int dw = s / P, f = s % P;
+    uint32_t x = (w[dw] >> (LO * f)) & mask;
+    if constexpr (B == 16) {
+      out[s >> 2][s & 3] = raw_to_half2(x, raw_bf);
+    } else {
+      if constexpr (HI != 0) {
+        // channels x0 = 2 P dw + f and x0 + P: their high parts, HI bits each, at bits HI x of the high run
+        constexpr uint32_t hmask = (1u << HI) - 1u;
+        const int at = HI * (2 * P * dw + f), next = at + HI * P;
+        x |= ((w[LO + at / 32] >> (at % 32)) & hmask) << LO;
+        x |= ((w[LO + next / 32] >> (next % 32)) & hmask) << (LO + 16);
+      }
+      out[s >> 2][s & 3] = as_u32(whole_to_half2(x));
+    }
+  }
+}
+
+// The fields of LO bits of four 16-channel tiles (tiles 4 half .. 4 half + 3) of a lane's piece of a value block: pair v of tile
+// t is words' field 4 t + v.  out[4 t + v]: two codes, tokens 2 v and 2 v + 1 of the lane's eight.
+template <int B> __device__ __forceinline__ void value_fields(const uint32_t* __restrict__ block, int lane, int half, uint32_t (&out)[16]) {
+  constexpr int P = 16 / B;
+  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << B) - 1u) * 0x00010001u;
+  uint32_t w[B];
+  if constexpr (B == 1) {
+    w[0] = block[2 * lane + half];
+  } else if constexpr (B == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(block + 4 * lane + 2 * half);
+    w[0] = x.x; w[1] = x.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < B / 4; ++i)
+      *reinterpret_cast<u32x4*>(w + 4 * i) = *reinterpret_cast<const u32x4*>(block + 256 * (B / 4 * half + i) + 4 * lane);
+  }
+#pragma unroll
+  for (int s = 0; s < 16; ++s) out[s] = (w[s / P] >> (B * (s % P))) & mask;
+}
+
+// What a workgroup walks: tokens [0, sink_tiles * 64) and [first * 64, ...), n tiles in all.
+struct Walk { int sink_tiles, first, n; };
+__device__ __forceinline__ Walk make_walk(int p_first, int p_last, int window, int sinks) {
+  Walk w;
+  const int lo = window ? max(p_first - window + 1, 0) : 0;
+  w.first = lo / kTileTokens;
+  w.sink_tiles = min((sinks + kTileTokens - 1) / kTileTokens, w.first);
+  w.n = p_last < 0 ? 0 : w.sink_tiles + (p_last / kTileTokens + 1 - w.first);
+  return w;
+}
+
+template <int NG>
+__global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t sm_tile[2 * kTileTokens * kHeadDim * 2];   // keys, then values
+  __shared__ __attribute__((aligned(16))) float sm_scale[4][kTileTokens];                      // key scales, by matrix row
+  __shared__ __attribute__((aligned(16))) uint32_t sm_zero[kTileTokens][4];                    // key zeros, each twice
+  __shared__ __attribute__((aligned(16))) uint32_t sm_qsum[kTileRows][4];                      // group sums of the query, two parts each
+  __shared__ float sm_kappa[kTileRows];
+  uint8_t* const sm_k = sm_tile;
+  uint8_t* const sm_v = sm_tile + kTileTokens * kHeadDim * 2;
+
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int b = blockIdx.x / g.kv_heads, h = blockIdx.x % g.kv_heads;
+  const int R = a.heads_per_kv;
+  const int len = a.seq_lens ? min(max(a.seq_lens[b], 0), a.seq_bound) : a.seq_bound;
+  const int nq = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
+  // later rows see more: they go first
+  const int split = blockIdx.z, tile = (int)gridDim.y - 1 - (int)blockIdx.y;
+  const int row0 = tile * kTileRows, rows = nq * R;
+  if (row0 >= rows) return;
+  const int row_end = min(row0 + kTileRows, rows);
+  const int p0 = len - nq;                               // position of query token 0
+  const int p_last = p0 + (row_end - 1) / R;
+  const Walk walk = make_walk(p0 + row0 / R, p_last, a.window, a.sinks);
+  const int per = (walk.n + a.splits - 1) / a.splits;
+  const int t_begin = split * per, t_end = min(t_begin + per, walk.n);
+  const int limit = p_last + 1;                          // no row of the tile sees a token from here on
+  const bool raw_bf = g.raw_dtype == KVQ_BF16;
+  // Reconstructions may lie past binary16's largest number (code * scale + zero with a scale that was rounded up): results that overflow
+  // become that number, half a step off, instead of infinity (FP16_OVFL, bit 23 of the MODE register).
+  __builtin_amdgcn_s_setreg(1 | (23 << 6), 1);
+
+  // ---- query: rows to binary16 in slot order through LDS (16 lanes a row), group sums, operands into registers
+  {
+    const int fields = key_fields(g.bits_k);
+    const int lane16 = tid & 15, d0 = 8 * lane16;
+    const uint32_t signs = rot_sign_bits(g.signs_k, lane16);
+    for (int it = 0; it < kTileRows / 16; ++it) {
+      const int r = 16 * it + (tid >> 4), row = min(row0 + r, rows - 1);
+      const int i = row / R, hq = h * R + row % R;
+      const uint4 raw = *reinterpret_cast<const uint4*>(a.q + (b * a.q_sb + i * a.q_st + hq * a.q_sh + d0));
+      const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = widen16((uint16_t)(rw[e >> 1] >> (16 * (e & 1))), a.q_bf16);
+      if (g.rotate_k) rotate8(x, lane16, signs);
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { x[e] = (float)(_Float16)x[e]; sum += x[e]; }
+      sum += lane_xor<1>(sum);
+      sum += lane_xor<2>(sum);
+      if (NG <= 2) sum += lane_xor<4>(sum);
+      if (NG == 1) sum += lane_xor<8>(sum);
+      // a row whose sums do not fit binary16 is scaled down by a power of two as a whole
+      float most = fabsf(sum);
+      if (NG == 4) most = fmaxf(most, lane_xor<4>(most));
+      if (NG >= 2) most = fmaxf(most, lane_xor<8>(most));
+      const int down = max((int)((__float_as_uint(most) >> 23) & 0xFF) - (127 + 14), 0);
+      const float unit = __uint_as_float((uint32_t)(127 - down) << 23);
+      uint8_t* dst = sm_tile + r * 256;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int slot = (d0 & ~31) + key_slot((d0 & 31) + e, fields);
+        const int at = (((slot >> 3) ^ (r & 15)) << 4) + (slot & 7) * 2;
+        *reinterpret_cast<_Float16*>(dst + at) = (_Float16)(x[e] * unit);
+      }
+      if (lane16 == 0) sm_kappa[r] = a.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 + down) << 23);
+      const int q = lane16 >> 2;                         // group q's sum: in lane 16 q / NG of the row (all lanes take part)
+      const float group_sum = __shfl(sum, (lane & ~15) + (NG == 1 ? 0 : NG == 2 ? 8 * (q & 1) : 4 * q));
+      if ((lane16 & 3) == 0) {
+        const float mine = q < NG ? group_sum * unit : 0.0f;
+        half2v parts;
+        parts[0] = (_Float16)mine;
+        parts[1] = (_Float16)(mine - (float)parts[0]);
+        sm_qsum[r][q] = as_u32(parts);
+      }
+    }
+  }
+  __syncthreads();
+  const int col = lane & 31, hh = lane >> 5;
+  const int my_row = wave * kRowsPerWave + col;
+  u32x4 qb[8], qs;
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk)
+    qb[kk] = *reinterpret_cast<const u32x4*>(sm_tile + my_row * 256 + (((2 * kk + hh) ^ (my_row & 15)) << 4));
+  qs = *reinterpret_cast<const u32x4*>(sm_qsum[my_row]);
+  if (hh) qs = u32x4{0u, 0u, 0u, 0u};
+  const float kappa = sm_kappa[my_row];
+  const int my_p = p0 + min(row0 + my_row, rows - 1) / R;                    // position of this lane's query
+  const int my_lo = a.window ? my_p - a.window : -1;                         // ... and the newest token that is too old for it
+  // the wavefront's positions, for the tiles that need no mask
+  const int w_first = p0 + min(row0 + wave * kRowsPerWave, rows - 1) / R, w_last = p0 + min(row0 + wave * kRowsPerWave + 31, rows - 1) / R;
+  __syncthreads();
+
+  float16v acc[4];
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
+  float m = kNoMax, l = 0.0f;
+
+  for (int ti = t_begin; ti < t_end; ++ti) {
+    const int t0 = (ti < walk.sink_tiles ? ti : walk.first + ti - walk.sink_tiles) * kTileTokens;
+    // ---- unpack the tile
+    // (paged: a tile never straddles a page)
+    const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0);      // plane order's number of the tile's first token
+    {
+      const int tok = tid >> 2, chunk = tid & 3;
+      const int src = min(t0 + tok, limit - 1) - t0;                           // (nothing behind the last visible token is read)
+      const int x = tok & 31, row = (tok & 32) | (x & 7) | ((x & 8) << 1) | ((x & 16) >> 1);   // bits 3 and 4 swapped
+      u32x4 piece[4];
+      const uint32_t* kp = (const uint32_t*)a.cache.k_codes + (base + src) * (4 * g.bits_k) + chunk * g.bits_k;
+      switch (g.bits_k) {
+        case 1: unpack_key_chunk<1>(kp, raw_bf, piece); break;
+        case 2: unpack_key_chunk<2>(kp, raw_bf, piece); break;
+        case 3: unpack_key_chunk<3>(kp, raw_bf, piece); break;
+        case 4: unpack_key_chunk<4>(kp, raw_bf, piece); break;
+        case 6: unpack_key_chunk<6>(kp, raw_bf, piece); break;
+        case 8: unpack_key_chunk<8>(kp, raw_bf, piece); break;
+        default: unpack_key_chunk<16>(kp, raw_bf, piece); break;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<u32x4*>(sm_k + row * 256 + (((4 * chunk + i) ^ (row & 15)) << 4)) = piece[i];
+      uint32_t meta = 0;
+      if (g.bits_k == 16) meta = 0x00003C00u;                                  // scale 1, zero 0
+      else if (chunk < NG) meta = ((const uint32_t*)a.cache.k_meta)[meta_index(base + src, chunk, NG)];
+      if (t0 + tok >= limit || chunk >= NG) meta = 0;
+      sm_scale[chunk][row] = widen16((uint16_t)meta, false);
+      sm_zero[row][chunk] = (meta >> 16) * 0x00010001u;
+    }
+    {
+      const int blk = tid >> 7, half = (tid >> 6) & 1;
+      const int sblk = min((t0 >> 5) + blk, (limit - 1) >> 5) - (t0 >> 5);
+      const uint32_t* vp = (const uint32_t*)a.cache.v_codes + ((base >> 5) + sblk) * (128 * g.bits_v);
+      uint32_t f[16];
+      switch (g.bits_v) {
+        case 1: value_fields<1>(vp, lane, half, f); break;
+        case 2: value_fields<2>(vp, lane, half, f); break;
+        case 4: value_fields<4>(vp, lane, half, f); break;
+        case 8: value_fields<8>(vp, lane, half, f); break;
+        case 16: value_fields<16>(vp, lane, half, f); break;
+        default: {                                         // 3 and 6 bits: a block of low parts, a block of high parts
+          uint32_t hi[16];
+          if (g.bits_v == 3) {
+            value_fields<2>(vp, lane, half, f); value_fields<1>(vp + 256, lane, half, hi);
+          } else {
+            value_fields<4>(vp, lane, half, f); value_fields<2>(vp + 512, lane, half, hi);
+          }
+          const int lo = g.bits_v == 3 ? 2 : 4;
+#pragma unroll
+          for (int s = 0; s < 16; ++s) f[s] |= hi[s] << lo;
+        }
+      }
+      const int j = lane >> 4, dl = lane & 15;
+      const int valid = limit - (t0 + 32 * blk + 4 * j);   // of tokens 16 x4 + 4 j + r those with 16 x4 + r < valid are visible to some row
+      if (g.bits_v == 16) {
+#pragma unroll
+        for (int s = 0; s < 16; ++s) {
+          const int at = 16 * ((s & 2) >> 1) + 2 * (s & 1);    // pair v = s % 4: tokens 2 v, 2 v + 1 of the eight (x4, r)
+          uint32_t x = raw_to_half2(f[s], raw_bf);
+          if (at >= valid) x &= 0xFFFF0000u;
+          if (at + 1 >= valid) x &= 0x0000FFFFu;
+          f[s] = x;
+        }
+      } else {
+        const int per_group = g.g_v >> 4;                  // 16-channel tiles of a group
+        u32x4 m4[2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int dt = 4 * half + t;
+          if (t == 0 || (t == 2 && per_group == 2)) {
+            const int gr = dt / per_group;
+            const uint32_t* mp = (const uint32_t*)a.cache.v_meta + meta_index(base + 32 * sblk, gr, g.ng_v) + 4 * j;
+#pragma unroll
+            for (int x4 = 0; x4 < 2; ++x4) {
+              m4[x4] = *reinterpret_cast<const u32x4*>(mp + 16 * g.ng_v * x4);
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (16 * x4 + r >= valid) m4[x4][r] = 0u;
+            }
+          }
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const uint32_t e0 = m4[v >> 1][2 * (v & 1)], e1 = m4[v >> 1][2 * (v & 1) + 1];
+            const half2v s = as_half2((e0 & 0xFFFFu) | (e1 << 16)), z = as_half2((e0 >> 16) | (e1 & 0xFFFF0000u));
+            f[4 * t + v] = as_u32(__builtin_elementwise_fma(whole_to_half2(f[4 * t + v]), s, z));
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        *reinterpret_cast<u32x4*>(sm_v + blk * 8192 + (j * 128 + 16 * (4 * half + t) + dl) * 16) =
+            u32x4{f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]};
+    }
+    __syncthreads();
+
+    // ---- two blocks of 32 tokens
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk) {
+      const int tb = t0 + 32 * blk;
+      if (tb > w_last) break;                              // uniform in the wavefront
+      const uint8_t* kt = sm_k + blk * 8192;
+      float16v s;
+      {
+        float16v zero;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
+        s = mma32(*reinterpret_cast<const u32x4*>(sm_zero[32 * blk + col]), qs, zero);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          float16v part = zero;
+#pragma unroll
+          for (int kk = n * (8 / NG); kk < (n + 1) * (8 / NG); ++kk)
+            part = mma32(*reinterpret_cast<const u32x4*>(kt + col * 256 + (((2 * kk + hh) ^ (col & 15)) << 4)), qb[kk], part);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4v sc = *reinterpret_cast<const float4v*>(&sm_scale[n][32 * blk + 8 * q + 4 * hh]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(sc[e], part[4 * q + e], s[4 * q + e]);
+          }
+        }
+      }
+      // register i: token 16 (i / 4 % 2) + 8 (i / 8) + 4 hh + i % 4 of the block
+      const bool whole = tb + 31 <= w_first && (a.window == 0 || tb > w_last - a.window);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int t = tb + 16 * ((i >> 2) & 1) + 8 * (i >> 3) + 4 * hh + (i & 3);
+          const bool seen = (t <= my_p) & ((t > my_lo) | (t < a.sinks));
+          s[i] = seen ? s[i] : -INFINITY;
+        }
+      }
+      float most = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+      most = fmaxf(most, other_half(most)) * kappa;
+      if (__any(most > m + kMaxSlack)) {
+        const float m_new = fmaxf(m, most), f = exp2f(m - m_new);
+        m = m_new;
+        l *= f;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[ct][i] *= f;
+      }
+      const float off = kWeightBits - m;
+      u32x4 pw[2];
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        half2v p;
+        p[0] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * v], kappa, off));
+        p[1] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], kappa, off));
+        l = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, l, false);
+        pw[v >> 2][v & 3] = as_u32(p);
+      }
+      const uint8_t* vt = sm_v + blk * 8192;
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+          acc[ct] = mma32(*reinterpret_cast<const u32x4*>(vt + ((2 * st + hh) * 128 + 32 * ct + col) * 16), pw[st], acc[ct]);
+    }
+    __syncthreads();
+  }
+
+  // ---- results.  acc[ct][i]: channel 32 ct + 8 (i / 4) + 4 hh + i % 4 of row `col`
+  l += other_half(l);
+  if (g.rotate_v) {                                        // back to the input basis: linear, so partial sums as well
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(i & 1)) { const float u = acc[ct][i], w = acc[ct][i + 1]; acc[ct][i] = u + w; acc[ct][i + 1] = u - w; }
+#pragma unroll
+    for (int step = 2; step <= 8; step <<= 1) {
+      if (step == 4) {                                     // stride 4 of the channels: the other half of the wavefront
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) { const float o = other_half(acc[ct][i]); acc[ct][i] = hh ? o - acc[ct][i] : acc[ct][i] + o; }
+      }
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!(i & step)) { const float u = acc[ct][i], w = acc[ct][i + step]; acc[ct][i] = u + w; acc[ct][i + step] = u - w; }
+    }
+#pragma unroll
+    for (int step = 1; step < 4; step <<= 1)
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct)
+        if (!(ct & step))
+#pragma unroll
+          for (int i = 0; i < 16; ++i) { const float u = acc[ct][i], w = acc[ct + step][i]; acc[ct][i] = u + w; acc[ct + step][i] = u - w; }
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int d = 8 * (i >> 2) + 4 * hh + (i & 3);
+        const float x = acc[ct][i] * kRotScale;
+        acc[ct][i] = (g.signs_v[ct] >> d) & 1u ? -x : x;
+      }
+  }
+  const int row = row0 + my_row;
+  if (row >= rows) return;
+  const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
+  if (a.splits > 1) {
+    float* rec = a.ws + (hq * a.splits + split) * kRec;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4v*>(rec + 32 * ct + 8 * q + 4 * hh) =
+            float4v{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
+    if (hh == 0) { rec[kHeadDim] = m; rec[kHeadDim + 1] = l; }
+    return;
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;            // (a row that sees nothing: zeros)
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t o = hq * kHeadDim + 32 * ct + 8 * q + 4 * hh;
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = acc[ct][4 * q + e] * inv;
+      if (a.out_dtype == KVQ_F32) *reinterpret_cast<float4v*>((float*)a.out + o) = float4v{y[0], y[1], y[2], y[3]};
+      else {
+        uint2 w;
+        if (a.out_dtype == KVQ_F16) {
+          half2v u; u[0] = (_Float16)y[0]; u[1] = (_Float16)y[1];
+          half2v t; t[0] = (_Float16)y[2]; t[1] = (_Float16)y[3];
+          w = make_uint2(as_u32(u), as_u32(t));
+        } else {
+          w = make_uint2(f32_to_bf16_bits(y[0]) | (uint32_t)f32_to_bf16_bits(y[1]) << 16, f32_to_bf16_bits(y[2]) | (uint32_t)f32_to_bf16_bits(y[3]) << 16);
+        }
+        *reinterpret_cast<uint2*>((uint16_t*)a.out + o) = w;
+      }
+    }
+}
+
+// Joins the partial records of a row: one wavefront a row, two channels a lane.
+__global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t hq = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (hq >= (int64_t)a.g.batch * a.n_q * a.q_heads) return;
+  const int i = (int)(hq / a.q_heads % a.n_q), b = (int)(hq / a.q_heads / a.n_q);
+  if (a.q_lens && i >= a.q_lens[b]) return;                // rows behind the sequence's last stay as they are
+  const float* rec = a.ws + hq * a.splits * kRec;
+  float m = kNoMax;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, rec[s * kRec + kHeadDim]);
+  float l = 0.0f, x = 0.0f, y = 0.0f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float f = exp2f(rec[s * kRec + kHeadDim] - m);
+    l += f * rec[s * kRec + kHeadDim + 1];
+    x += f * rec[s * kRec + 2 * lane];
+    y += f * rec[s * kRec + 2 * lane + 1];
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  x *= inv; y *= inv;
+  const int64_t o = hq * kHeadDim + 2 * lane;
+  if (a.out_dtype == KVQ_F32) *reinterpret_cast<float2*>((float*)a.out + o) = make_float2(x, y);
+  else if (a.out_dtype == KVQ_F16) { half2v u; u[0] = (_Float16)x; u[1] = (_Float16)y; *reinterpret_cast<uint32_t*>((uint16_t*)a.out + o) = as_u32(u); }
+  else *reinterpret_cast<uint32_t*>((uint16_t*)a.out + o) = f32_to_bf16_bits(x) | (uint32_t)f32_to_bf16_bits(y) << 16;
+}
+
+}  // namespace
+
+// How many parts the tokens of a row tile are cut into: enough workgroups for two per compute unit, at least 4 tiles each.
+int32_t plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks) {
+  const int64_t tiles = ((int64_t)n_q * heads_per_kv + kTileRows - 1) / kTileRows * g.batch * g.kv_heads;
+  int64_t span = seq_bound;
+  if (window) span = span < (int64_t)window + sinks + n_q ? span : (int64_t)window + sinks + n_q;
+  const int64_t steps = (span + kTileTokens - 1) / kTileTokens;
+  int64_t splits = (2 * device_compute_units() + tiles - 1) / tiles;
+  if (splits > steps / 4) splits = steps / 4;
+  return (int32_t)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+}
+size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits) {
+  return splits <= 1 ? 0 : (size_t)batch * n_q * q_heads * splits * kRec * sizeof(float);
+}
+
+hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t stream) {
+  const int tiles = (a.n_q * a.heads_per_kv + kTileRows - 1) / kTileRows;
+  const dim3 grid(a.g.batch * a.g.kv_heads, tiles, a.splits);
+  switch (a.g.ng_k) {
+    case 1: hipLaunchKernelGGL((chunk_kernel<1>), grid, dim3(64 * kWaves), 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((chunk_kernel<2>), grid, dim3(64 * kWaves), 0, stream, a); break;
+    case 4: hipLaunchKernelGGL((chunk_kernel<4>), grid, dim3(64 * kWaves), 0, stream, a); break;
+    default: return hipErrorInvalidValue;
+  }
+  if (a.splits > 1) {
+    const int64_t rows = (int64_t)a.g.batch * a.n_q * a.q_heads;
+    hipLaunchKernelGGL(chunk_merge_kernel, dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace kvq

@@ -126,6 +126,33 @@ struct DecodeArgs {
   const uint16_t* k_new; const uint16_t* v_new; int in_bf16; int64_t nsb, nsh;
 };
 
+// Everything the kernels of several query tokens per sequence need, passed by value (kvq_chunk_attention, kvq_window_attention).
+struct ChunkArgs {
+  Geom g;
+  kvq_cache cache;
+  const uint16_t* q; int q_bf16; int64_t q_sb, q_st, q_sh;      // element strides of batch, query token, head
+  int32_t q_heads, heads_per_kv, n_q;
+  const int32_t* q_lens;          // per sequence, clamped to [0, n_q]; nullptr: n_q
+  const int32_t* seq_lens;        // per sequence, clamped to [0, seq_bound]; nullptr: seq_bound
+  int32_t seq_bound, window, sinks;
+  float softmax_scale;
+  void* out; int out_dtype;       // [B][n_q][q_heads][D]
+  float* ws; int32_t splits;      // parts a row's tokens are cut into; > 1: partial records in ws, joined by a second launch
+};
+int32_t plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks);
+size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits);
+hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t stream);
+
+// Append of several tokens per sequence with the rotation of their positions (kvq_rope_append).
+struct RopeArgs {
+  Geom g;
+  kvq_cache cache;
+  const uint16_t* q; uint16_t* q_out; int64_t q_sb, q_st, q_sh; int32_t q_heads, heads_per_kv;
+  const uint16_t* k_new; const uint16_t* v_new; int64_t sb, sh, st;
+  const int32_t* pos; const int32_t* n_tokens; int32_t n_new, capacity;      // capacity: tokens at positions from here on are left out
+  const float* cos_t; const float* sin_t; int32_t rotary, interleaved;
+};
+hipError_t launch_rope_append(const RopeArgs& a, int in_dtype, hipStream_t stream);
 
 // Launchers (each validates nothing: the C ABI layer has done it).  Return hipGetLastError().
 hipError_t launch_quantize_append(const Geom& g, const kvq_cache& c, const void* k_new, const void* v_new,

@@ -43,6 +43,10 @@ class _CCache(C.Structure):
                                           "v_scale_exp")]
 
 
+class _CRope(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("rows", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
 _lib = None
 # The extension module with the hot calls (csrc/kvq_binding.cpp).  Its functions take what the functions below take and return the
 # library's status, or None for a case that they leave to the code here.
@@ -112,11 +116,23 @@ def load():
         lib.kvq_reconstruction_error.argtypes = [C.POINTER(_CLayout), C.POINTER(_CCache), C.c_void_p, C.c_void_p, C.c_int,
                                                  C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         lib.kvq_selftest_quantizer.argtypes = [C.c_void_p, C.c_void_p]
+        lib.kvq_rope_append.argtypes = [C.POINTER(_CLayout), C.POINTER(_CCache), C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                        C.c_void_p, C.c_int32, C.POINTER(_CRope), C.c_void_p]
+        lib.kvq_chunk_workspace_bytes.argtypes = [C.POINTER(_CLayout), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                                  C.POINTER(C.c_size_t)]
+        lib.kvq_window_workspace_bytes.argtypes = [C.POINTER(_CLayout), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.kvq_chunk_attention.argtypes = [C.POINTER(_CLayout), C.POINTER(_CCache), C.c_void_p, C.c_int, C.c_int32, C.c_int64, C.c_int64,
+                                            C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_float,
+                                            C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.kvq_window_attention.argtypes = [C.POINTER(_CLayout), C.POINTER(_CCache), C.c_void_p, C.c_int, C.c_int32, C.c_void_p, C.c_int32,
+                                             C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.kvq_status_string.argtypes = [C.c_int]
         lib.kvq_status_string.restype = C.c_char_p
         for f in ("kvq_cache_bytes", "kvq_residual_bytes", "kvq_decode_workspace_bytes", "kvq_quantize_append", "kvq_decode_attention",
                   "kvq_decode_step", "kvq_dequantize", "kvq_reconstruction_error", "kvq_decode_attention_varlen",
-                  "kvq_decode_step_varlen", "kvq_selftest_quantizer", "kvq_decode_attention_static"):
+                  "kvq_decode_step_varlen", "kvq_selftest_quantizer", "kvq_decode_attention_static", "kvq_rope_append", "kvq_chunk_workspace_bytes",
+                  "kvq_window_workspace_bytes", "kvq_chunk_attention", "kvq_window_attention"):
             getattr(lib, f).restype = C.c_int
         _bind(lib)
         _lib = lib
@@ -397,4 +413,91 @@ def decode_step_varlen(layout: Layout, cache: Cache, k_new: torch.Tensor, v_new:
                                        softmax_scale, _p(out), _DTYPES[out.dtype], _p(workspace),
                                        _nbytes(workspace), _stream_ptr())
     _check(st, "kvq_decode_step_varlen")
+    return out
+
+
+# ---- several tokens per sequence ---------------------------------------------------------------------------------------------
+
+class Rope:
+    """The rotation of positions: cos and sin, float32 device tensors [positions, rotary_dim / 2].  interleaved: channel 2i pairs with
+    2i + 1, otherwise channel i with i + rotary_dim / 2."""
+
+    def __init__(self, cos: torch.Tensor, sin: torch.Tensor, interleaved: bool = False):
+        assert cos.dim() == 2 and cos.shape == sin.shape and cos.dtype == sin.dtype == torch.float32
+        assert cos.is_contiguous() and sin.is_contiguous() and cos.device == sin.device
+        self.cos, self.sin, self.interleaved = cos, sin, bool(interleaved)
+        self._struct = _CRope(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(self.interleaved))
+
+    def c(self) -> _CRope:
+        return self._struct
+
+
+def _lens_ok(t, layout: Layout) -> bool:
+    return t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == layout.batch)
+
+
+def rope_append(layout: Layout, cache: Cache, q, k_new: torch.Tensor, v_new: torch.Tensor, pos: torch.Tensor, rope: Rope,
+                q_out=None, n_tokens=None):
+    """Append k_new, v_new ([B, H_kv, n, D] fp16/bf16, last axis contiguous) to every sequence at its own position pos[b] (int32 device
+    tensor [B]; n_tokens, likewise, where sequences bring fewer than n), keys rotated by their positions' angles.  q: [B, n, H_q, D] of
+    the same type (last axis contiguous), rotated into q_out (contiguous, of q's shape; q itself where q is contiguous; made here when it
+    is None), or None.  Returns q_out."""
+    shape, strides, dtype = k_new.shape, k_new.stride(), k_new.dtype
+    assert shape == v_new.shape and dtype == v_new.dtype and len(shape) == 4 and shape[:2] == (layout.batch, layout.kv_heads)
+    assert shape[3] == layout.head_dim and strides == v_new.stride() and strides[3] == 1
+    assert pos is not None and _lens_ok(pos, layout) and _lens_ok(n_tokens, layout)
+    qs, heads = (0, 0, 0, 1), 0
+    if q is not None:
+        heads, qs = q.size(2), q.stride()
+        assert q.dim() == 4 and q.shape == (shape[0], shape[2], heads, shape[3]) and q.dtype == dtype and qs[3] == 1
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        assert q_out.shape == q.shape and q_out.dtype == dtype and q_out.is_contiguous()
+    else:
+        assert q_out is None
+    st = load().kvq_rope_append(layout.c(), cache.c(), _p(q), qs[0], qs[1], qs[2], heads, _p(q_out), k_new.data_ptr(), v_new.data_ptr(),
+                                _DTYPES[dtype], strides[0], strides[1], strides[2], pos.data_ptr(), _p(n_tokens), shape[2], rope.c(),
+                                _stream_ptr())
+    _check(st, "kvq_rope_append")
+    return q_out
+
+
+def chunk_workspace_bytes(layout: Layout, q_heads: int, n_q: int, max_seq_len: int, window: int = 0, sinks: int = 0) -> int:
+    out = C.c_size_t()
+    _check(load().kvq_chunk_workspace_bytes(layout.c(), q_heads, n_q, max_seq_len, window, sinks, C.byref(out)), "kvq_chunk_workspace_bytes")
+    return int(out.value)
+
+
+def chunk_attention(layout: Layout, cache: Cache, q: torch.Tensor, q_lens, seq_lens, max_seq_len: int, window: int, sinks: int,
+                    softmax_scale: float, out: torch.Tensor, workspace) -> torch.Tensor:
+    """Causal attention of the last tokens of every sequence over its cache.  q: [B, n_q, H_q, D] fp16/bf16, last axis contiguous; out:
+    contiguous fp32/fp16/bf16 of q's shape; q_lens, seq_lens: int32 device tensors [B] (None: n_q and max_seq_len for all); window: newest
+    tokens a query sees, its own among them (0: all); sinks: first tokens it sees besides; workspace: uint8 device tensor or None."""
+    shape, strides = q.shape, q.stride()
+    assert len(shape) == 4 and shape[0] == layout.batch and shape[3] == layout.head_dim and strides[3] == 1
+    assert out.is_contiguous() and out.shape == shape and _lens_ok(q_lens, layout) and _lens_ok(seq_lens, layout)
+    st = load().kvq_chunk_attention(layout.c(), cache.c(), q.data_ptr(), _DTYPES[q.dtype], shape[2], strides[0], strides[1], strides[2],
+                                    shape[1], _p(q_lens), _p(seq_lens), max_seq_len, window, sinks, softmax_scale, out.data_ptr(),
+                                    _DTYPES[out.dtype], _p(workspace), _nbytes(workspace), _stream_ptr())
+    _check(st, "kvq_chunk_attention")
+    return out
+
+
+def window_workspace_bytes(layout: Layout, q_heads: int, max_seq_len: int, window: int, sinks: int) -> int:
+    out = C.c_size_t()
+    _check(load().kvq_window_workspace_bytes(layout.c(), q_heads, max_seq_len, window, sinks, C.byref(out)), "kvq_window_workspace_bytes")
+    return int(out.value)
+
+
+def window_attention(layout: Layout, cache: Cache, q: torch.Tensor, seq_lens, max_seq_len: int, window: int, sinks: int,
+                     softmax_scale: float, out: torch.Tensor, workspace) -> torch.Tensor:
+    """decode_attention_varlen with a sliding window and sinks: the query of sequence b (position seq_lens[b] - 1) sees its newest
+    `window` tokens (0: all) and the first `sinks`.  q, out: [B, H_q, D] contiguous; seq_lens: int32 device tensor [B] or None."""
+    shape = q.shape
+    assert q.is_contiguous() and out.is_contiguous() and len(shape) == 3 and out.shape == shape and _lens_ok(seq_lens, layout)
+    assert shape[0] == layout.batch and shape[2] == layout.head_dim
+    st = load().kvq_window_attention(layout.c(), cache.c(), q.data_ptr(), _DTYPES[q.dtype], shape[1], _p(seq_lens), max_seq_len, window,
+                                     sinks, softmax_scale, out.data_ptr(), _DTYPES[out.dtype], _p(workspace), _nbytes(workspace),
+                                     _stream_ptr())
+    _check(st, "kvq_window_attention")
     return out
