@@ -46,6 +46,10 @@ UNITS = [("kvq_api.hip", "kvq_api.o", []),
          ("kvq_decode.hip", "kvq_decode.o", [])]
 UNITS += [("kvq_decode.hip", f"kvq_decode_k{bk}v{bv}.o",
            [f"-DKVQ_INST_BK={bk}", f"-DKVQ_INST_BV={bv}", "-Rpass-analysis=kernel-resource-usage"]) for bk, bv in DECODE_PAIRS]
+# the kernel for a few query rows over every pair of widths, one unit each
+WIDTHS = (1, 2, 3, 4, 6, 8, 16)
+UNITS += [("kvq_few.hip", f"kvq_few_k{bk}v{bv}.o",
+           [f"-DKVQ_INST_BK={bk}", f"-DKVQ_INST_BV={bv}", "-Rpass-analysis=kernel-resource-usage"]) for bk in WIDTHS for bv in WIDTHS]
 
 
 def _compile(item):

@@ -358,11 +358,12 @@ kvq_status chunk_common(const kvq_layout* layout, const kvq_cache* cache, const 
   a.window = window; a.sinks = sinks; a.softmax_scale = softmax_scale;
   a.out = out; a.out_dtype = out_dtype;
   a.ws = (float*)workspace;
-  a.splits = kvq::plan_chunk(a.g, a.heads_per_kv, n_q, max_seq_len, window, sinks);
+  const kvq::ChunkPlan plan = kvq::plan_chunk(a.g, a.heads_per_kv, n_q, max_seq_len, window, sinks);
+  a.splits = plan.splits;
   const size_t record = kvq::chunk_record_bytes(layout->batch, n_q, q_heads, 2) / 2;
   const size_t room = workspace ? workspace_bytes / record : 0;
   if ((size_t)a.splits > room) a.splits = room < 2 ? 1 : (int32_t)room;
-  return kvq::launch_chunk_attention(a, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+  return kvq::launch_chunk_attention(a, plan.few_sets, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 }  // namespace
 
@@ -373,7 +374,7 @@ kvq_status kvq_chunk_workspace_bytes(const kvq_layout* layout, int32_t q_heads, 
   if (!bytes_out) return KVQ_ERR_INVALID_ARG;
   const kvq::Geom g = kvq::make_geom(*layout);
   *bytes_out = n_q == 0 ? 0 : kvq::chunk_record_bytes(layout->batch, n_q, q_heads,
-                                                      kvq::plan_chunk(g, q_heads / layout->kv_heads, n_q, max_seq_len, window, sinks));
+                                                      kvq::plan_chunk(g, q_heads / layout->kv_heads, n_q, max_seq_len, window, sinks).splits);
   return KVQ_OK;
 }
 

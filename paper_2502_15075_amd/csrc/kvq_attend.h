@@ -1,0 +1,121 @@
+// What the attention kernels of several query tokens per sequence share: operand types, unpacking of codes into binary16, the staging of
+// the query.
+#pragma once
+#include "kvq_internal.h"
+#include "kvq_quantizer.h"
+
+namespace kvq {
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNoMax = -1.0e30f;
+constexpr int kRec = kHeadDim + 4;       // floats of a partial record: 128 sums, maximum, weight sum
+
+__device__ __forceinline__ half2v as_half2(uint32_t x) { return __builtin_bit_cast(half2v, x); }
+__device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ float other_half(float x) {           // lane ^ 32's value
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+// two whole numbers below 1024 in the halves of x -> the same as binary16
+__device__ __forceinline__ half2v whole_to_half2(uint32_t x) {
+  return as_half2(x | 0x64006400u) - half2v{(_Float16)1024.0f, (_Float16)1024.0f};
+}
+// Two patterns of the unquantized type -> binary16 (bfloat16: exact in binary16's normal range)
+__device__ __forceinline__ uint32_t raw_to_half2(uint32_t x, bool bf) {
+  if (!bf) return x;
+  half2v h;
+  h[0] = (_Float16)__uint_as_float(x << 16);
+  h[1] = (_Float16)__uint_as_float(x & 0xFFFF0000u);
+  return as_u32(h);
+}
+
+// Channel order inside a 32-channel chunk of an unpacked key row: with P = 16 / (field width), field pair (p, p + P) of dword w is
+// slots 2 (w P + p) and + 1.  The slot of channel x (0..31):
+__device__ __forceinline__ int key_slot(int x, int per) {
+  const int w = x / (2 * per), rem = x % (2 * per);
+  return 2 * (w * per + rem % per) + rem / per;
+}
+__device__ __forceinline__ int key_fields(int bits) { return bits == 3 ? 8 : bits == 6 ? 4 : 16 / bits; }
+
+// Query rows [row0, row0 + n) of a kv head (row = query token * heads_per_kv + head; rows behind the last repeat it) to LDS, by 16 lanes a
+// row: binary16 in slot order, 256 bytes a row whose 16-byte pieces are permuted by the row's number (piece p at p ^ (r & 15)); the sums of
+// ng equal parts of the row (4 at most), each as two binary16 parts (`parts`, may be null) or in binary32 (`sums`, may be null); and the factor of the row's scores.
+template <int THREADS>
+__device__ __forceinline__ void stage_query(const ChunkArgs& a, int b, int h, int row0, int rows, int n, int ng, uint8_t* dst, uint32_t (*parts)[4],
+                                            float (*sums)[4], float* kappa) {
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63, lane16 = tid & 15, d0 = 8 * lane16, R = a.heads_per_kv;
+  const int fields = key_fields(g.bits_k);
+  // (read out one by one: a choice among words of the argument block may become a table in private memory)
+  uint32_t words[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) words[i] = __builtin_amdgcn_readfirstlane(g.signs_k[i]);
+  const int w = lane16 >> 2;
+  const uint32_t signs = ((w == 0 ? words[0] : w == 1 ? words[1] : w == 2 ? words[2] : words[3]) >> (8 * (lane16 & 3))) & 0xFFu;
+  for (int r = tid >> 4; r < n; r += THREADS / 16) {
+    const int row = min(row0 + r, rows - 1);
+    const int i = row / R, hq = h * R + row % R;
+    const uint4 raw = *reinterpret_cast<const uint4*>(a.q + (b * a.q_sb + i * a.q_st + hq * a.q_sh + d0));
+    const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = widen16((uint16_t)(rw[e >> 1] >> (16 * (e & 1))), a.q_bf16);
+    if (g.rotate_k) rotate8(x, lane16, signs);
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { x[e] = (float)(_Float16)x[e]; sum += x[e]; }
+    sum += lane_xor<1>(sum);
+    sum += lane_xor<2>(sum);
+    if (ng <= 2) sum += lane_xor<4>(sum);
+    if (ng == 1) sum += lane_xor<8>(sum);
+    // a row whose sums do not fit binary16 is scaled down by a power of two as a whole
+    float most = fabsf(sum);
+    if (ng == 4) most = fmaxf(most, lane_xor<4>(most));
+    if (ng >= 2) most = fmaxf(most, lane_xor<8>(most));
+    const int down = max((int)((__float_as_uint(most) >> 23) & 0xFF) - (127 + 14), 0);
+    const float unit = __uint_as_float((uint32_t)(127 - down) << 23);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int slot = (d0 & ~31) + key_slot((d0 & 31) + e, fields);
+      const int at = (((slot >> 3) ^ (r & 15)) << 4) + (slot & 7) * 2;
+      *reinterpret_cast<_Float16*>(dst + r * 256 + at) = (_Float16)(x[e] * unit);
+    }
+    if (lane16 == 0) kappa[r] = a.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 + down) << 23);
+    const int q = lane16 >> 2;                         // part q's sum: in lane 16 q / ng of the row (all lanes take part)
+    const float group_sum = __shfl(sum, (lane & ~15) + (ng == 1 ? 0 : ng == 2 ? 8 * (q & 1) : 4 * q));
+    if ((lane16 & 3) == 0) {
+      const float mine = q < ng ? group_sum * unit : 0.0f;
+      half2v p;
+      p[0] = (_Float16)mine;
+      p[1] = (_Float16)(mine - (float)p[0]);
+      if (parts) parts[r][q] = as_u32(p);
+      if (sums) sums[r][q] = mine;
+    }
+  }
+}
+
+// One output element group: four neighbouring channels at element o in the caller's type (16-bit types: rounded once).
+__device__ __forceinline__ void store_out4(void* out, int out_dtype, int64_t o, const float (&y)[4]) {
+  if (out_dtype == KVQ_F32) *reinterpret_cast<float4v*>((float*)out + o) = float4v{y[0], y[1], y[2], y[3]};
+  else {
+    uint2 w;
+    if (out_dtype == KVQ_F16) {
+      half2v u, t;
+      u[0] = (_Float16)y[0]; u[1] = (_Float16)y[1]; t[0] = (_Float16)y[2]; t[1] = (_Float16)y[3];
+      w = make_uint2(as_u32(u), as_u32(t));
+    } else {
+      w = make_uint2(f32_to_bf16_bits(y[0]) | (uint32_t)f32_to_bf16_bits(y[1]) << 16, f32_to_bf16_bits(y[2]) | (uint32_t)f32_to_bf16_bits(y[3]) << 16);
+    }
+    *reinterpret_cast<uint2*>((uint16_t*)out + o) = w;
+  }
+}
+
+}  // namespace
+}  // namespace kvq

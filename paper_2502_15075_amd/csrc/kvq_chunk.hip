@@ -14,55 +14,20 @@
 // query are too), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are rounded alike).  Key scales
 // are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the query's
 // group sums, each split into two binary16 parts.
-#include "kvq_internal.h"
-#include "kvq_quantizer.h"
+#include "kvq_attend.h"
+#include "kvq_few.h"
 
 namespace kvq {
 namespace {
 
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-typedef _Float16 half8v __attribute__((ext_vector_type(8)));
-typedef float float4v __attribute__((ext_vector_type(4)));
-typedef float float16v __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNoMax = -1.0e30f;
 constexpr float kWeightBits = 10.0f;     // weights carry 2^10: small ones stay clear of binary16's subnormals
 constexpr float kMaxSlack = 4.0f;        // the running maximum is raised once it lags by more: weights stay below 2^14
 constexpr int kTileTokens = 64;
 constexpr int kRowsPerWave = 32, kWaves = 4, kTileRows = kRowsPerWave * kWaves;
-constexpr int kRec = kHeadDim + 4;       // floats of a partial record: 128 sums, maximum, weight sum
 
 __device__ __forceinline__ float16v mma32(u32x4 a, u32x4 b, float16v c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ half2v as_half2(uint32_t x) { return __builtin_bit_cast(half2v, x); }
-__device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast(uint32_t, x); }
-__device__ __forceinline__ float other_half(float x) {           // lane ^ 32's value
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
-}
-// two whole numbers below 1024 in the halves of x -> the same as binary16
-__device__ __forceinline__ half2v whole_to_half2(uint32_t x) {
-  return as_half2(x | 0x64006400u) - half2v{(_Float16)1024.0f, (_Float16)1024.0f};
-}
-// Two patterns of the unquantized type -> binary16 (bfloat16: exact in binary16's normal range)
-__device__ __forceinline__ uint32_t raw_to_half2(uint32_t x, bool bf) {
-  if (!bf) return x;
-  half2v h;
-  h[0] = (_Float16)__uint_as_float(x << 16);
-  h[1] = (_Float16)__uint_as_float(x & 0xFFFF0000u);
-  return as_u32(h);
-}
-
-// Channel order inside a 32-channel chunk of an unpacked key row: with P = 16 / (field width), field pair (p, p + P) of dword w is
-// slots 2 (w P + p) and + 1.  The slot of channel x (0..31):
-__device__ __forceinline__ int key_slot(int x, int per) {
-  const int w = x / (2 * per), rem = x % (2 * per);
-  return 2 * (w * per + rem % per) + rem / per;
-}
-__device__ __forceinline__ int key_fields(int bits) { return bits == 3 ? 8 : bits == 6 ? 4 : 16 / bits; }
 
 // The codes of one 32-channel chunk (B dwords at p) as 16 binary16 pairs in slot order, four 16-byte pieces.
 template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* __restrict__ p, bool raw_bf, u32x4 (&out)[4]) {
@@ -139,7 +104,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
 
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = blockIdx.x / g.kv_heads, h = blockIdx.x % g.kv_heads;
+  // (a division leaves its result in vector registers, and with it every address: these are the same in all lanes)
+  const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / g.kv_heads), h = blockIdx.x - b * g.kv_heads;
   const int R = a.heads_per_kv;
   const int len = a.seq_lens ? min(max(a.seq_lens[b], 0), a.seq_bound) : a.seq_bound;
   const int nq = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
@@ -149,9 +115,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
   if (row0 >= rows) return;
   const int row_end = min(row0 + kTileRows, rows);
   const int p0 = len - nq;                               // position of query token 0
-  const int p_last = p0 + (row_end - 1) / R;
-  const Walk walk = make_walk(p0 + row0 / R, p_last, a.window, a.sinks);
-  const int per = (walk.n + a.splits - 1) / a.splits;
+  const int p_last = p0 + __builtin_amdgcn_readfirstlane((row_end - 1) / R);
+  const Walk walk = make_walk(p0 + __builtin_amdgcn_readfirstlane(row0 / R), p_last, a.window, a.sinks);
+  const int per = __builtin_amdgcn_readfirstlane((walk.n + a.splits - 1) / a.splits);
   const int t_begin = split * per, t_end = min(t_begin + per, walk.n);
   const int limit = p_last + 1;                          // no row of the tile sees a token from here on
   const bool raw_bf = g.raw_dtype == KVQ_BF16;
@@ -159,52 +125,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
   // become that number, half a step off, instead of infinity (FP16_OVFL, bit 23 of the MODE register).
   __builtin_amdgcn_s_setreg(1 | (23 << 6), 1);
 
-  // ---- query: rows to binary16 in slot order through LDS (16 lanes a row), group sums, operands into registers
-  {
-    const int fields = key_fields(g.bits_k);
-    const int lane16 = tid & 15, d0 = 8 * lane16;
-    const uint32_t signs = rot_sign_bits(g.signs_k, lane16);
-    for (int it = 0; it < kTileRows / 16; ++it) {
-      const int r = 16 * it + (tid >> 4), row = min(row0 + r, rows - 1);
-      const int i = row / R, hq = h * R + row % R;
-      const uint4 raw = *reinterpret_cast<const uint4*>(a.q + (b * a.q_sb + i * a.q_st + hq * a.q_sh + d0));
-      const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = widen16((uint16_t)(rw[e >> 1] >> (16 * (e & 1))), a.q_bf16);
-      if (g.rotate_k) rotate8(x, lane16, signs);
-      float sum = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) { x[e] = (float)(_Float16)x[e]; sum += x[e]; }
-      sum += lane_xor<1>(sum);
-      sum += lane_xor<2>(sum);
-      if (NG <= 2) sum += lane_xor<4>(sum);
-      if (NG == 1) sum += lane_xor<8>(sum);
-      // a row whose sums do not fit binary16 is scaled down by a power of two as a whole
-      float most = fabsf(sum);
-      if (NG == 4) most = fmaxf(most, lane_xor<4>(most));
-      if (NG >= 2) most = fmaxf(most, lane_xor<8>(most));
-      const int down = max((int)((__float_as_uint(most) >> 23) & 0xFF) - (127 + 14), 0);
-      const float unit = __uint_as_float((uint32_t)(127 - down) << 23);
-      uint8_t* dst = sm_tile + r * 256;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int slot = (d0 & ~31) + key_slot((d0 & 31) + e, fields);
-        const int at = (((slot >> 3) ^ (r & 15)) << 4) + (slot & 7) * 2;
-        *reinterpret_cast<_Float16*>(dst + at) = (_Float16)(x[e] * unit);
-      }
-      if (lane16 == 0) sm_kappa[r] = a.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 + down) << 23);
-      const int q = lane16 >> 2;                         // group q's sum: in lane 16 q / NG of the row (all lanes take part)
-      const float group_sum = __shfl(sum, (lane & ~15) + (NG == 1 ? 0 : NG == 2 ? 8 * (q & 1) : 4 * q));
-      if ((lane16 & 3) == 0) {
-        const float mine = q < NG ? group_sum * unit : 0.0f;
-        half2v parts;
-        parts[0] = (_Float16)mine;
-        parts[1] = (_Float16)(mine - (float)parts[0]);
-        sm_qsum[r][q] = as_u32(parts);
-      }
-    }
-  }
+  stage_query<64 * kWaves>(a, b, h, row0, rows, kTileRows, NG, sm_tile, sm_qsum, nullptr, sm_kappa);
   __syncthreads();
   const int col = lane & 31, hh = lane >> 5;
   const int my_row = wave * kRowsPerWave + col;
@@ -218,7 +139,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
   const int my_p = p0 + min(row0 + my_row, rows - 1) / R;                    // position of this lane's query
   const int my_lo = a.window ? my_p - a.window : -1;                         // ... and the newest token that is too old for it
   // the wavefront's positions, for the tiles that need no mask
-  const int w_first = p0 + min(row0 + wave * kRowsPerWave, rows - 1) / R, w_last = p0 + min(row0 + wave * kRowsPerWave + 31, rows - 1) / R;
+  const int w_first = p0 + __builtin_amdgcn_readfirstlane(min(row0 + wave * kRowsPerWave, rows - 1) / R);
+  const int w_last = p0 + __builtin_amdgcn_readfirstlane(min(row0 + wave * kRowsPerWave + 31, rows - 1) / R);
   __syncthreads();
 
   float16v acc[4];
@@ -454,18 +376,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
       float y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = acc[ct][4 * q + e] * inv;
-      if (a.out_dtype == KVQ_F32) *reinterpret_cast<float4v*>((float*)a.out + o) = float4v{y[0], y[1], y[2], y[3]};
-      else {
-        uint2 w;
-        if (a.out_dtype == KVQ_F16) {
-          half2v u; u[0] = (_Float16)y[0]; u[1] = (_Float16)y[1];
-          half2v t; t[0] = (_Float16)y[2]; t[1] = (_Float16)y[3];
-          w = make_uint2(as_u32(u), as_u32(t));
-        } else {
-          w = make_uint2(f32_to_bf16_bits(y[0]) | (uint32_t)f32_to_bf16_bits(y[1]) << 16, f32_to_bf16_bits(y[2]) | (uint32_t)f32_to_bf16_bits(y[3]) << 16);
-        }
-        *reinterpret_cast<uint2*>((uint16_t*)a.out + o) = w;
-      }
+      store_out4(a.out, a.out_dtype, o, y);
     }
 }
 
@@ -496,28 +407,54 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
 
 }  // namespace
 
-// How many parts the tokens of a row tile are cut into: enough workgroups for two per compute unit, at least 4 tiles each.
-int32_t plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks) {
-  const int64_t tiles = ((int64_t)n_q * heads_per_kv + kTileRows - 1) / kTileRows * g.batch * g.kv_heads;
-  int64_t span = seq_bound;
-  if (window) span = span < (int64_t)window + sinks + n_q ? span : (int64_t)window + sinks + n_q;
-  const int64_t steps = (span + kTileTokens - 1) / kTileTokens;
-  int64_t splits = (2 * device_compute_units() + tiles - 1) / tiles;
-  if (splits > steps / 4) splits = steps / 4;
-  return (int32_t)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+// Up to kFewRowsMax rows of a kv head go to the kernel that keeps the cache packed, more to the tiles above.  The tokens are cut into parts
+// where there are fewer workgroups than compute units, as long as a part leaves every wavefront a few steps.
+constexpr int kFewRowsMax = 128;
+ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks) {
+  ChunkPlan plan{0, 1};
+  const int64_t rows = (int64_t)n_q * heads_per_kv, streams = (int64_t)g.batch * g.kv_heads;
+  int64_t span = seq_bound, splits;
+  if (window && span > (int64_t)window + sinks + n_q) span = (int64_t)window + sinks + n_q;
+  if (rows <= kFewRowsMax) {
+    plan.few_sets = rows <= 16 ? 1 : 2;
+    const int64_t groups = streams * ((rows + 16 * plan.few_sets - 1) / (16 * plan.few_sets)), blocks = (span + 31) / 32;
+    splits = device_compute_units() / groups;
+    if (splits > blocks / 16) splits = blocks / 16;
+  } else {
+    const int64_t tiles = (rows + kTileRows - 1) / kTileRows * streams, steps = (span + kTileTokens - 1) / kTileTokens;
+    splits = (2 * device_compute_units() + tiles - 1) / tiles;
+    if (splits > steps / 4) splits = steps / 4;
+  }
+  plan.splits = (int32_t)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+  return plan;
 }
 size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits) {
   return splits <= 1 ? 0 : (size_t)batch * n_q * q_heads * splits * kRec * sizeof(float);
 }
 
-hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t stream) {
-  const int tiles = (a.n_q * a.heads_per_kv + kTileRows - 1) / kTileRows;
-  const dim3 grid(a.g.batch * a.g.kv_heads, tiles, a.splits);
-  switch (a.g.ng_k) {
-    case 1: hipLaunchKernelGGL((chunk_kernel<1>), grid, dim3(64 * kWaves), 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((chunk_kernel<2>), grid, dim3(64 * kWaves), 0, stream, a); break;
-    case 4: hipLaunchKernelGGL((chunk_kernel<4>), grid, dim3(64 * kWaves), 0, stream, a); break;
-    default: return hipErrorInvalidValue;
+namespace {
+hipError_t launch_few(const ChunkArgs& a, int32_t sets, hipStream_t stream) {
+  switch (32 * a.g.bits_k + a.g.bits_v) {
+#define KVQ_FEW_CASE(k, v) case 32 * k + v: return launch_few_k##k##v##v(a, sets, stream);
+    KVQ_FEW_PAIRS(KVQ_FEW_CASE)
+  }
+  return hipErrorInvalidValue;
+}
+}  // namespace
+
+hipError_t launch_chunk_attention(const ChunkArgs& a, int32_t few_sets, hipStream_t stream) {
+  if (few_sets) {
+    const hipError_t e = launch_few(a, few_sets, stream);
+    if (e != hipSuccess) return e;
+  } else {
+    const int tiles = (a.n_q * a.heads_per_kv + kTileRows - 1) / kTileRows;
+    const dim3 grid(a.g.batch * a.g.kv_heads, tiles, a.splits);
+    switch (a.g.ng_k) {
+      case 1: hipLaunchKernelGGL((chunk_kernel<1>), grid, dim3(64 * kWaves), 0, stream, a); break;
+      case 2: hipLaunchKernelGGL((chunk_kernel<2>), grid, dim3(64 * kWaves), 0, stream, a); break;
+      case 4: hipLaunchKernelGGL((chunk_kernel<4>), grid, dim3(64 * kWaves), 0, stream, a); break;
+      default: return hipErrorInvalidValue;
+    }
   }
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.g.batch * a.n_q * a.q_heads;

@@ -139,9 +139,11 @@ struct ChunkArgs {
   void* out; int out_dtype;       // [B][n_q][q_heads][D]
   float* ws; int32_t splits;      // parts a row's tokens are cut into; > 1: partial records in ws, joined by a second launch
 };
-int32_t plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks);
+// How such a call is run: few_sets != 0: the kernel for a few rows, with that many column sets of 16 rows a workgroup; 0: tiles of rows.
+struct ChunkPlan { int32_t few_sets, splits; };
+ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks);
 size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits);
-hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t stream);
+hipError_t launch_chunk_attention(const ChunkArgs& a, int32_t few_sets, hipStream_t stream);
 
 // Append of several tokens per sequence with the rotation of their positions (kvq_rope_append).
 struct RopeArgs {

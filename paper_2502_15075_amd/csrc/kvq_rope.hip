@@ -120,7 +120,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const RopeArgs a) {
   static_assert(stage_total<16, kRopeSpan>() >= stage_total<6, kRopeSpan>(), "staging area");
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane16 = tid & 15, d0 = 8 * lane16;
-  const int b = blockIdx.y / g.kv_heads, h = blockIdx.y % g.kv_heads;
+  // (a division leaves its result in vector registers, and with it every address: these are the same in all lanes)
+  const int b = __builtin_amdgcn_readfirstlane(blockIdx.y / g.kv_heads), h = blockIdx.y - b * g.kv_heads;
   const int pos = a.pos[b];
   const int count = a.n_tokens ? min(max(a.n_tokens[b], 0), a.n_new) : a.n_new;
   const int first = max(pos, 0), end = (int)min((int64_t)pos + count, (int64_t)a.capacity);    // positions that are stored
