@@ -23,9 +23,12 @@ __device__ __forceinline__ float other_half(float x) {           // lane ^ 32's 
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
-// two whole numbers below 1024 in the halves of x -> the same as binary16
-__device__ __forceinline__ half2v whole_to_half2(uint32_t x) {
-  return as_half2(x | 0x64006400u) - half2v{(_Float16)1024.0f, (_Float16)1024.0f};
+// Two whole numbers below 1024 in the halves of x (masked out of it) -> the same as binary16: the pattern of 1024 + x, less 1024.
+// `one_k` is that pattern, 1024 in both halves, in a vector register of its own: mask and pattern together are then one instruction, which
+// takes no two constants.
+__device__ __forceinline__ uint32_t one_k_pattern() { uint32_t x = 0x64006400u; asm("" : "+v"(x)); return x; }
+__device__ __forceinline__ half2v whole_to_half2(uint32_t x, uint32_t mask, uint32_t one_k) {
+  return as_half2((x & mask) | one_k) - half2v{(_Float16)1024.0f, (_Float16)1024.0f};
 }
 // Two patterns of the unquantized type -> binary16 (bfloat16: exact in binary16's normal range)
 __device__ __forceinline__ uint32_t raw_to_half2(uint32_t x, bool bf) {

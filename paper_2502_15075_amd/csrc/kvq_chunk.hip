@@ -30,7 +30,7 @@ __device__ __forceinline__ float16v mma32(u32x4 a, u32x4 b, float16v c) {
 }
 
 // The codes of one 32-channel chunk (B dwords at p) as 16 binary16 pairs in slot order, four 16-byte pieces.
-template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* __restrict__ p, bool raw_bf, u32x4 (&out)[4]) {
+template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* __restrict__ p, bool raw_bf, uint32_t one_k, u32x4 (&out)[4]) {
   constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
   constexpr int P = 16 / LO;                       // pairs per dword
   constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
@@ -45,7 +45,7 @@ template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t
 #pragma unroll
   for (int s = 0; s < 16; ++s) {
     const int dw = s / P, f = s % P;
-    uint32_t x = (w[dw] >> (LO * f)) & mask;
+    uint32_t x = w[dw] >> (LO * f);
     if constexpr (B == 16) {
       out[s >> 2][s & 3] = raw_to_half2(x, raw_bf);
     } else {
@@ -53,17 +53,19 @@ template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t
         // channels x0 = 2 P dw + f and x0 + P: their high parts, HI bits each, at bits HI x of the high run
         constexpr uint32_t hmask = (1u << HI) - 1u;
         const int at = HI * (2 * P * dw + f), next = at + HI * P;
+        x &= mask;
         x |= ((w[LO + at / 32] >> (at % 32)) & hmask) << LO;
         x |= ((w[LO + next / 32] >> (next % 32)) & hmask) << (LO + 16);
       }
-      out[s >> 2][s & 3] = as_u32(whole_to_half2(x));
+      out[s >> 2][s & 3] = as_u32(whole_to_half2(x, HI != 0 ? ~0u : mask, one_k));
     }
   }
 }
 
 // The fields of LO bits of four 16-channel tiles (tiles 4 half .. 4 half + 3) of a lane's piece of a value block: pair v of tile
 // t is words' field 4 t + v.  out[4 t + v]: two codes, tokens 2 v and 2 v + 1 of the lane's eight.
-template <int B> __device__ __forceinline__ void value_fields(const uint32_t* __restrict__ block, int lane, int half, uint32_t (&out)[16]) {
+// MASKED: cut to the field (what is joined with high parts).
+template <int B, bool MASKED = false> __device__ __forceinline__ void value_fields(const uint32_t* __restrict__ block, int lane, int half, uint32_t (&out)[16]) {
   constexpr int P = 16 / B;
   constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << B) - 1u) * 0x00010001u;
   uint32_t w[B];
@@ -78,7 +80,7 @@ template <int B> __device__ __forceinline__ void value_fields(const uint32_t* __
       *reinterpret_cast<u32x4*>(w + 4 * i) = *reinterpret_cast<const u32x4*>(block + 256 * (B / 4 * half + i) + 4 * lane);
   }
 #pragma unroll
-  for (int s = 0; s < 16; ++s) out[s] = (w[s / P] >> (B * (s % P))) & mask;
+  for (int s = 0; s < 16; ++s) out[s] = MASKED ? (w[s / P] >> (B * (s % P))) & mask : w[s / P] >> (B * (s % P));
 }
 
 // What a workgroup walks: tokens [0, sink_tiles * 64) and [first * 64, ...), n tiles in all.
@@ -149,6 +151,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
   float m = kNoMax, l = 0.0f;
+  const uint32_t one_k = one_k_pattern(), v_mask = ((1u << min(g.bits_v, 15)) - 1u) * 0x00010001u;
 
   for (int ti = t_begin; ti < t_end; ++ti) {
     const int t0 = (ti < walk.sink_tiles ? ti : walk.first + ti - walk.sink_tiles) * kTileTokens;
@@ -162,13 +165,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
       u32x4 piece[4];
       const uint32_t* kp = (const uint32_t*)a.cache.k_codes + (base + src) * (4 * g.bits_k) + chunk * g.bits_k;
       switch (g.bits_k) {
-        case 1: unpack_key_chunk<1>(kp, raw_bf, piece); break;
-        case 2: unpack_key_chunk<2>(kp, raw_bf, piece); break;
-        case 3: unpack_key_chunk<3>(kp, raw_bf, piece); break;
-        case 4: unpack_key_chunk<4>(kp, raw_bf, piece); break;
-        case 6: unpack_key_chunk<6>(kp, raw_bf, piece); break;
-        case 8: unpack_key_chunk<8>(kp, raw_bf, piece); break;
-        default: unpack_key_chunk<16>(kp, raw_bf, piece); break;
+        case 1: unpack_key_chunk<1>(kp, raw_bf, one_k, piece); break;
+        case 2: unpack_key_chunk<2>(kp, raw_bf, one_k, piece); break;
+        case 3: unpack_key_chunk<3>(kp, raw_bf, one_k, piece); break;
+        case 4: unpack_key_chunk<4>(kp, raw_bf, one_k, piece); break;
+        case 6: unpack_key_chunk<6>(kp, raw_bf, one_k, piece); break;
+        case 8: unpack_key_chunk<8>(kp, raw_bf, one_k, piece); break;
+        default: unpack_key_chunk<16>(kp, raw_bf, one_k, piece); break;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -194,9 +197,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
         default: {                                         // 3 and 6 bits: a block of low parts, a block of high parts
           uint32_t hi[16];
           if (g.bits_v == 3) {
-            value_fields<2>(vp, lane, half, f); value_fields<1>(vp + 256, lane, half, hi);
+            value_fields<2, true>(vp, lane, half, f); value_fields<1, true>(vp + 256, lane, half, hi);
           } else {
-            value_fields<4>(vp, lane, half, f); value_fields<2>(vp + 512, lane, half, hi);
+            value_fields<4, true>(vp, lane, half, f); value_fields<2, true>(vp + 512, lane, half, hi);
           }
           const int lo = g.bits_v == 3 ? 2 : 4;
 #pragma unroll
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
           for (int v = 0; v < 4; ++v) {
             const uint32_t e0 = m4[v >> 1][2 * (v & 1)], e1 = m4[v >> 1][2 * (v & 1) + 1];
             const half2v s = as_half2((e0 & 0xFFFFu) | (e1 << 16)), z = as_half2((e0 >> 16) | (e1 & 0xFFFF0000u));
-            f[4 * t + v] = as_u32(__builtin_elementwise_fma(whole_to_half2(f[4 * t + v]), s, z));
+            f[4 * t + v] = as_u32(__builtin_elementwise_fma(whole_to_half2(f[4 * t + v], v_mask, one_k), s, z));
           }
         }
       }
@@ -416,9 +419,11 @@ ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_b
   int64_t span = seq_bound, splits;
   if (window && span > (int64_t)window + sinks + n_q) span = (int64_t)window + sinks + n_q;
   if (rows <= kFewRowsMax) {
-    plan.few_sets = rows <= 16 ? 1 : 2;
-    const int64_t groups = streams * ((rows + 16 * plan.few_sets - 1) / (16 * plan.few_sets)), blocks = (span + 31) / 32;
-    splits = device_compute_units() / groups;
+    const int ngk = g.bits_k == 16 ? 1 : g.ng_k, ngv = g.bits_v == 16 ? 1 : g.ng_v;
+    const int most = few_max_sets(g.bits_k, g.bits_v, ngk > ngv ? ngk : ngv), sets = (int)((rows + 15) / 16);
+    plan.few_sets = (sets + (sets + most - 1) / most - 1) / ((sets + most - 1) / most);         // as few row tiles as can be, of the same size
+    const int64_t groups = streams * ((sets + plan.few_sets - 1) / plan.few_sets), blocks = (span + 31) / 32;
+    splits = (plan.few_sets == 1 ? 2 : 1) * device_compute_units() / groups;
     if (splits > blocks / 16) splits = blocks / 16;
   } else {
     const int64_t tiles = (rows + kTileRows - 1) / kTileRows * streams, steps = (span + kTileTokens - 1) / kTileTokens;

@@ -4,22 +4,27 @@
 
 namespace kvq {
 
-constexpr int kFewRows = 32;                       // rows (query token, query head) of a workgroup, in column sets of 16
+// Column sets of 16 rows (query token, query head) a workgroup takes at most: three where their sums and a block's registers fit.
+constexpr int few_max_sets(int bits_k, int bits_v, int groups) { return bits_k + bits_v <= 8 && groups <= 2 ? 3 : 2; }
+constexpr int kFewWaves = 8;
 
 template <int B> constexpr int key_loads() { return (32 * B + 63) / 64; }            // 16-byte loads of a lane for 32 key rows
-template <int BK, int BV> constexpr int few_step_regs() { return 4 * key_loads<BK>() + 2 * BV + 4; }
-// wavefronts of a workgroup: eight, four where the registers or the LDS of eight would not fit
-template <int BK, int BV, int NC> constexpr int few_waves() { return BK + BV > 16 ? 4 : 8; }
-// steps in flight per wavefront
-template <int BK, int BV, int NC> constexpr int few_stages() { return NC == 1 && few_step_regs<BK, BV>() <= 40 ? 2 : 1; }
-template <int BK, int BV> constexpr int few_wave_bytes() { return 1024 * key_loads<BK>() + (BK == 16 && BV == 16 ? 0 : 1024); }
+// Wavefronts per SIMD that the registers are cut for (512 of them a SIMD): the sums take 32 per column set, the next block 2 (b_K + b_V), the
+// rest about 80.
+template <int BK, int BV, int NC, int NG> constexpr int few_occupancy() {
+  constexpr bool odd = BK == 3 || BK == 6 || BV == 3 || BV == 6 || BK == 1 || BV == 1;          // (codes in two runs, lanes that share a word)
+  return NC > 1 || BK + BV > 16 || (NG == 4 && BK + BV > 12) ? 2 : NG == 4 || odd || BK + BV > 8 || (NG == 1 && BK + BV > 6) ? 3 : 4;
+}
+// LDS of a wavefront: a block's keys, values, scales and zeros
+template <int BK, int BV> constexpr int few_wave_bytes() { return 512 * BK + 512 * BV + (BK == 16 && BV == 16 ? 0 : 1024); }
+// the wavefronts' sums are joined through LDS in so many parts
+template <int NC> constexpr int few_join_parts() { return NC > 2 ? 2 : 1; }
 template <int BK, int BV, int NC> constexpr int few_lds_bytes() {
-  constexpr int NW = few_waves<BK, BV, NC>();
-  constexpr int walk = NW * few_wave_bytes<BK, BV>(), join = NW / 2 * NC * 64 * 38 * 4, query = 16 * NC * 256;
-  return walk > join ? (walk > query ? walk : query) : (join > query ? join : query);
+  constexpr int walk = kFewWaves * few_wave_bytes<BK, BV>(), join = kFewWaves * 16 * NC * (kHeadDim / few_join_parts<NC>() + 4) * 4;
+  return walk > join ? walk : join;
 }
 
-// One launcher per pair of widths (the units of kvq_few.hip); sets: column sets of 16 rows a workgroup takes, 1 or 2.
+// One launcher per pair of widths (the units of kvq_few.hip); sets: column sets of 16 rows a workgroup takes, 1 to few_max_sets.
 #define KVQ_FEW_VALUES(X, k) X(k, 1) X(k, 2) X(k, 3) X(k, 4) X(k, 6) X(k, 8) X(k, 16)
 #define KVQ_FEW_PAIRS(X) KVQ_FEW_VALUES(X, 1) KVQ_FEW_VALUES(X, 2) KVQ_FEW_VALUES(X, 3) KVQ_FEW_VALUES(X, 4) KVQ_FEW_VALUES(X, 6) \
   KVQ_FEW_VALUES(X, 8) KVQ_FEW_VALUES(X, 16)
@@ -46,6 +51,39 @@ template <int B> __device__ __forceinline__ void load_value_piece(uint32_t* w, c
       const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(block + ((1024u * i + 16u * lane) & live)));
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+    }
+  }
+}
+// The same piece, stored in and read from a block in LDS.
+template <int B> __device__ __forceinline__ void store_value_piece(const uint32_t* w, uint8_t* block, int lane) {
+  if constexpr (B == 3) {
+    store_value_piece<2>(w, block, lane);
+    store_value_piece<1>(w + 4, block + 1024, lane);
+  } else if constexpr (B == 6) {
+    store_value_piece<4>(w, block, lane);
+    store_value_piece<2>(w + 8, block + 2048, lane);
+  } else if constexpr (B == 1) {
+    *reinterpret_cast<uint2*>(block + 8 * lane) = make_uint2(w[0], w[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < B / 2; ++i) *reinterpret_cast<uint4*>(block + 1024 * i + 16 * lane) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+template <int B> __device__ __forceinline__ void read_value_piece(uint32_t* w, const uint8_t* block, int lane) {
+  if constexpr (B == 3) {
+    read_value_piece<2>(w, block, lane);
+    read_value_piece<1>(w + 4, block + 1024, lane);
+  } else if constexpr (B == 6) {
+    read_value_piece<4>(w, block, lane);
+    read_value_piece<2>(w + 8, block + 2048, lane);
+  } else if constexpr (B == 1) {
+    const uint2 x = *reinterpret_cast<const uint2*>(block + 8 * lane);
+    w[0] = x.x; w[1] = x.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < B / 2; ++i) {
+      const uint4 x = *reinterpret_cast<const uint4*>(block + 1024 * i + 16 * lane);
+      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
     }
   }
 }

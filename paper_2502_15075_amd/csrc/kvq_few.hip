@@ -12,8 +12,13 @@
 // output in binary32.  A weight is rounded to binary16 once, together with its value scale; for binary32 outputs (FINE) it
 // travels as two binary16 parts, 2^-22 of it.
 //
-// Key rows pass through a wavefront's own LDS: a lane needs 8 channels of every 32 of its token (all groups alike), which would be loads
-// of a few bytes.  Their 16-byte units are permuted by the row's number so that the reads meet no bank twice.
+// A code stays a number in the low bits of a binary16 lane, i.e. a subnormal: c 2^(k - 24) with its lowest bit at bit k, so that unpacking is a
+// shift and a mask; the power of two goes into the scores' factor and the final sums.  The matrix unit takes a subnormal by the exponent
+// 2^-14 and loses what lies 24 bits below a sum's largest product; k = 4 to 6 for narrow codes keeps that below binary32's own rounding.
+//
+// A wavefront's next block is on its way while it computes one: its loads land in registers, and go from there through LDS of the
+// wavefront's own at the start of the next turn.  A lane needs 8 channels of every 32 of its key row (all groups alike), which would be loads
+// of a few bytes; the rows' 16-byte units are permuted by the row's number so that the reads meet no bank twice.
 #include "kvq_attend.h"
 #include "kvq_few.h"
 
@@ -46,58 +51,79 @@ __device__ __forceinline__ float meta_z(uint32_t m) { return (float)as_half2(m)[
 template <int B> constexpr bool key_swizzled() { return (B & (B - 1)) == 0 && B > 1; }
 template <int B> __device__ __forceinline__ int key_swizzle(int row) { return key_swizzled<B>() ? (row * B / 16) & (B - 1) : 0; }
 
+// Where the lowest bit of a code lies in its binary16 lane.
+template <int B> constexpr int code_base() { return B == 1 || B == 2 ? 6 : B == 3 || B == 4 || B == 6 ? 4 : 0; }
+template <int B> constexpr float code_unit() { return B == 16 ? 1.0f : 1.0f / (float)(1 << (24 - code_base<B>())); }
+// x >> n, n < 0: x << -n
+template <int N> __device__ __forceinline__ uint32_t shifted(uint32_t x) { return N >= 0 ? x >> (N >= 0 ? N : 0) : x << (N < 0 ? -N : 0); }
+// Fields of W bits at bits AT and 16 + AT of x, their lowest bits taken to BASE and 16 + BASE
+template <int W, int AT, int BASE> __device__ __forceinline__ uint32_t field(uint32_t x) {
+  return shifted<AT - BASE>(x) & (((1u << W) - 1u) * 0x00010001u << BASE);
+}
+
 // Operand of channels 32 kk .. 32 kk + 31 of token row `row`: this lane's eight (slots 8 j .. 8 j + 7 of the chunk).
 template <int B> __device__ __forceinline__ u32x4 key_operand(const uint8_t* st, int row, int sw, int kk, int j, bool raw_bf) {
-  constexpr uint32_t mask = B == 16 ? 0u : ((1u << (B == 3 ? 2 : B == 6 ? 4 : B)) - 1u) * 0x00010001u;
+  constexpr int K = code_base<B>();
   const uint8_t* base = st + row * (16 * B);
-  u32x4 out;
   if constexpr (B == 16) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(base + (((4 * kk + j) ^ sw) << 4));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = raw_to_half2(w[i], raw_bf);
+    return u32x4{raw_to_half2(w[0], raw_bf), raw_to_half2(w[1], raw_bf), raw_to_half2(w[2], raw_bf), raw_to_half2(w[3], raw_bf)};
   } else if constexpr (B == 8) {
     const uint2 w = *reinterpret_cast<const uint2*>(base + (((2 * kk + (j >> 1)) ^ sw) << 4) + 8 * (j & 1));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = as_u32(whole_to_half2(((i >> 1 ? w.y : w.x) >> (8 * (i & 1))) & mask));
+    return u32x4{field<8, 0, K>(w.x), field<8, 8, K>(w.x), field<8, 0, K>(w.y), field<8, 8, K>(w.y)};
   } else if constexpr (B == 4 || B == 2 || B == 1) {
     const uint32_t w = B == 4 ? *reinterpret_cast<const uint32_t*>(base + ((kk ^ sw) << 4) + 4 * j)
                      : B == 2 ? *reinterpret_cast<const uint32_t*>(base + (((kk >> 1) ^ sw) << 4) + 8 * (kk & 1) + 4 * (j >> 1)) >> (8 * (j & 1))
                               : *reinterpret_cast<const uint32_t*>(base + 4 * kk) >> (4 * j);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = as_u32(whole_to_half2((w >> (B * i)) & mask));
+    return u32x4{field<B, 0, K>(w), field<B, B, K>(w), field<B, 2 * B, K>(w), field<B, 3 * B, K>(w)};
   } else if constexpr (B == 3) {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(base) + 3 * kk;
     const uint32_t lo = w[j >> 1] >> (8 * (j & 1)), hi = w[2] >> (16 * (j >> 1) + 4 * (j & 1));
+    u32x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      out[i] = as_u32(whole_to_half2(((lo >> (2 * i)) & mask) | (((hi >> i) & 1u) << 2) | (((hi >> (i + 8)) & 1u) << 18)));
+      out[i] = (((lo >> (2 * i)) & 0x00030003u) | (((hi >> i) & 1u) << 2) | (((hi >> (i + 8)) & 1u) << 18)) << K;
+    return out;
   } else {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(base) + 6 * kk;
     const uint32_t lo = w[j], hi = w[4 + (j >> 1)] >> (16 * (j & 1));
+    u32x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      out[i] = as_u32(whole_to_half2(((lo >> (4 * i)) & mask) | (((hi >> (2 * i)) & 3u) << 4) | (((hi >> (2 * i + 8)) & 3u) << 20)));
+      out[i] = (((lo >> (4 * i)) & 0x000F000Fu) | (((hi >> (2 * i)) & 3u) << 4) | (((hi >> (2 * i + 8)) & 3u) << 20)) << K;
+    return out;
   }
-  return out;
 }
 
 // ---- value blocks: a lane's piece, 2 b dwords; field 4 dt + v is pair v (tokens 2 v, 2 v + 1 of the lane's eight) of channel tile dt
-template <int B> __device__ __forceinline__ uint32_t value_field(const uint32_t* w, int q) {
-  constexpr int P = 16 / B;
-  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << B) - 1u) * 0x00010001u;
-  return (w[q / P] >> (B * (q % P))) & mask;
-}
 template <int B> __device__ __forceinline__ u32x4 value_operand(const uint32_t* w, int dt) {
-  u32x4 out;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const int q = 4 * dt + v;
-    if constexpr (B == 16) out[v] = w[q];
-    else if constexpr (B == 3) out[v] = as_u32(whole_to_half2(value_field<2>(w, q) | (value_field<1>(w + 4, q) << 2)));
-    else if constexpr (B == 6) out[v] = as_u32(whole_to_half2(value_field<4>(w, q) | (value_field<2>(w + 8, q) << 4)));
-    else out[v] = as_u32(whole_to_half2(value_field<B>(w, q)));
+  constexpr int K = code_base<B>();
+  if constexpr (B == 16) return u32x4{w[4 * dt], w[4 * dt + 1], w[4 * dt + 2], w[4 * dt + 3]};
+  else if constexpr (B == 8) return u32x4{field<8, 0, K>(w[2 * dt]), field<8, 8, K>(w[2 * dt]), field<8, 0, K>(w[2 * dt + 1]), field<8, 8, K>(w[2 * dt + 1])};
+  else if constexpr (B == 4) return u32x4{field<4, 0, K>(w[dt]), field<4, 4, K>(w[dt]), field<4, 8, K>(w[dt]), field<4, 12, K>(w[dt])};
+  else if constexpr (B == 2) {
+    const uint32_t x = w[dt >> 1];
+    return dt & 1 ? u32x4{field<2, 8, K>(x), field<2, 10, K>(x), field<2, 12, K>(x), field<2, 14, K>(x)}
+                  : u32x4{field<2, 0, K>(x), field<2, 2, K>(x), field<2, 4, K>(x), field<2, 6, K>(x)};
+  } else if constexpr (B == 1) {
+    const uint32_t x = w[dt >> 2] >> (4 * (dt & 3));
+    return u32x4{field<1, 0, K>(x), field<1, 1, K>(x), field<1, 2, K>(x), field<1, 3, K>(x)};
+  } else if constexpr (B == 3) {
+    const uint32_t x = w[dt >> 1] >> (8 * (dt & 1)), y = w[4 + (dt >> 2)] >> (4 * (dt & 3));
+    return u32x4{field<2, 0, K>(x) | field<1, 0, K + 2>(y), field<2, 2, K>(x) | field<1, 1, K + 2>(y), field<2, 4, K>(x) | field<1, 2, K + 2>(y),
+                 field<2, 6, K>(x) | field<1, 3, K + 2>(y)};
+  } else {
+    const uint32_t x = w[dt], y = w[8 + (dt >> 1)] >> (8 * (dt & 1));
+    return u32x4{field<4, 0, K>(x) | field<2, 0, K + 4>(y), field<4, 4, K>(x) | field<2, 2, K + 4>(y), field<4, 8, K>(x) | field<2, 4, K + 4>(y),
+                 field<4, 12, K>(x) | field<2, 6, K + 4>(y)};
   }
-  return out;
+}
+
+// Byte offset of a lane's i-th 16-byte load of 32 key rows (off: those of the first loads, after which the permutation repeats).
+template <int BK, int N> __device__ __forceinline__ uint32_t key_load_offset(const uint32_t (&off)[N], int i, int lane) {
+  if constexpr (BK == 1) return off[0];
+  else if constexpr (BK == 3) return i == 0 ? off[0] : 1024u + 16u * min(lane, 31);
+  else return off[i % N] + 1024u * (i / N * N);
 }
 
 template <int BK, int BV> struct Step {
@@ -108,13 +134,16 @@ template <int BK, int BV> struct Step {
 
 // NG: the larger number of groups per row of the two tensors; a tensor with fewer is taken as one with NG whose scales repeat.
 template <int BK, int BV, int NC, int NG, bool FINE>
-__global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(const ChunkArgs a) {
-  constexpr int NW = few_waves<BK, BV, NC>(), NK = key_loads<BK>(), ST = few_stages<BK, BV, NC>();
-  constexpr int kWaveBytes = few_wave_bytes<BK, BV>();
+__global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())) void few_kernel(const ChunkArgs a) {
+  constexpr int NW = kFewWaves, NK = key_loads<BK>(), kWaveBytes = few_wave_bytes<BK, BV>();
   constexpr bool RAWK = BK == 16, RAWV = BV == 16;
+  constexpr bool kQueryInLds = NC > 1;
+  constexpr float kUnitK = code_unit<BK>(), kUnitV = code_unit<BV>();
   __shared__ __attribute__((aligned(16))) uint8_t sm[few_lds_bytes<BK, BV, NC>()];
+  __shared__ __attribute__((aligned(16))) uint8_t sm_query[16 * NC * 256];
   __shared__ __attribute__((aligned(16))) float sm_sums[16 * NC][4];
-  __shared__ float sm_kappa[16 * NC];
+  __shared__ int sm_pos[16 * NC];                          // positions of the rows
+  __shared__ float sm_kappa[16 * NC], sm_m[NW][16 * NC], sm_l[NW][16 * NC];
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, j = lane >> 4;
@@ -135,74 +164,82 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
   const int lo = a.window ? max(p_first - a.window + 1, 0) : 0;
   const int first = lo >> 5, sink_blocks = min((a.sinks + 31) >> 5, first);
   const int n_blocks = p_last >= 0 ? sink_blocks + (p_last >> 5) + 1 - first : 0;
-  const int per = __builtin_amdgcn_readfirstlane((n_blocks + a.splits - 1) / a.splits);
+  const int per = a.splits == 1 ? n_blocks : __builtin_amdgcn_readfirstlane((n_blocks + a.splits - 1) / a.splits);
   const int begin = split * per, end = min(begin + per, n_blocks);
-  const int n_my = begin + wave < end ? (int)((unsigned)(end - begin - wave + NW - 1) / NW) : 0;
-  auto block_of = [&](int i) { const int x = begin + wave + NW * i; return x < sink_blocks ? x : x - sink_blocks + first; };
+  auto block_at = [&](int x) { return x < sink_blocks ? x : x - sink_blocks + first; };
 
   // ---- loads of a step
   const int nmk = RAWK ? 0 : 8 * g.ng_k, nmv = RAWV ? 0 : 8 * g.ng_v;        // 16-byte units of scales and zeros
-  uint32_t k_off[NK];
+  // (64 units are 64 / BK rows; the permutation of the units repeats every 16 rows)
+  constexpr int kRepeat = BK == 8 ? 2 : BK == 16 ? 4 : 1;
+  uint32_t k_off[kRepeat];
 #pragma unroll
-  for (int i = 0; i < NK; ++i) {
+  for (int i = 0; i < kRepeat; ++i) {
     const int u = min(64 * i + lane, 32 * BK - 1), row = u / BK;
     k_off[i] = (uint32_t)(row * BK + ((u % BK) ^ key_swizzle<BK>(row))) * 16;
   }
   const int mu = min(lane, nmk + nmv - 1);
+  const int meta_token = 16 * (mu < nmk ? mu >= 4 * g.ng_k : mu - nmk >= 4 * g.ng_v) + 4 * (mu & 3);      // the first token of this lane's unit
   const uint8_t* const meta_base = mu < nmk ? (const uint8_t*)a.cache.k_meta : (const uint8_t*)a.cache.v_meta;
-  const int meta_step = mu < nmk ? 128 * g.ng_k : 128 * g.ng_v, meta_off = 16 * (mu < nmk ? mu : mu - nmk);
+  const uint32_t meta_step = mu < nmk ? 128 * g.ng_k : 128 * g.ng_v, meta_off = 16 * (mu < nmk ? mu : mu - nmk);
   typedef const __attribute__((address_space(4))) int32_t* TablePtr;
   const TablePtr pages = (TablePtr)(uintptr_t)(g.page_shift ? a.cache.page_table + (int64_t)b * g.pages_per_seq : nullptr);
   const int page_blocks = g.page_shift - 5;
   auto page_of = [&](int blk) -> int { return g.page_shift ? pages[blk >> page_blocks] : 0; };
   // (live = 0: a step that is not there; its loads collapse to one line)
   auto load = [&](Step<BK, BV>& s, int blk, int page, uint32_t live) {
-    const int64_t vb = g.page_shift ? (((int64_t)page * g.kv_heads + h) << page_blocks) + (blk & ((1 << page_blocks) - 1))
-                                    : ((int64_t)b * g.kv_heads + h) * (g.t_cap >> 5) + blk;
+    const int64_t vb_ = g.page_shift ? (((int64_t)page * g.kv_heads + h) << page_blocks) + (blk & ((1 << page_blocks) - 1))
+                                     : ((int64_t)b * g.kv_heads + h) * (g.t_cap >> 5) + blk;
+    // (the choice above would leave the address in vector registers)
+    const int64_t vb = ((int64_t)__builtin_amdgcn_readfirstlane((int)(vb_ >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)vb_);
     const uint8_t* kp = (const uint8_t*)a.cache.k_codes + vb * (512 * BK);
     const uint8_t* vp = (const uint8_t*)a.cache.v_codes + vb * (512 * BV);
 #pragma unroll
-    for (int i = 0; i < NK; ++i) s.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + (k_off[i] & live)));
+    for (int i = 0; i < NK; ++i) s.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + (key_load_offset<BK>(k_off, i, lane) & live)));
     load_value_piece<BV>(s.v, vp, lane, live);
     if constexpr (RAWK && RAWV) s.meta = u32x4{0u, 0u, 0u, 0u};
-    else
-      s.meta = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(meta_base + vb * meta_step + (meta_off & live)));
+    else s.meta = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(meta_base + vb * meta_step + (meta_off & live)));
   };
 
-  Step<BK, BV> ring[ST];
-  if (n_my > 0) {
-#pragma unroll
-    for (int s = 0; s < ST; ++s) {
-      const int blk = block_of(s < n_my ? s : 0);
-      load(ring[s], blk, page_of(blk), s < n_my ? ~0u : 0u);
-    }
-  }
+  Step<BK, BV> step;
+  const int x0 = begin + wave;                             // this wavefront's blocks: x0, x0 + NW, ...
+  if (x0 < end) load(step, block_at(x0), page_of(block_at(x0)), ~0u);
+  int page = x0 + NW < end ? page_of(block_at(x0 + NW)) : 0;
+  const int scale_exp = RAWV ? 0 : a.cache.v_scale_exp[(int64_t)b * g.kv_heads + h];
 
   // ---- query
-  stage_query<64 * NW>(a, b, h, row0, rows, 16 * NC, NG, sm, nullptr, sm_sums, sm_kappa);
+  stage_query<64 * NW>(a, b, h, row0, rows, 16 * NC, NG, sm_query, nullptr, sm_sums, sm_kappa);
+  if (tid < 16 * NC) sm_pos[tid] = p0 + min(row0 + tid, rows - 1) / R;
   __syncthreads();
-  u32x4 qb[NC][4];
-  float qsum[NC][NG], kappa[NC];
-  int my_p[NC];
+  auto query_operand = [&](int cs, int kk) { return *reinterpret_cast<const u32x4*>(sm_query + (16 * cs + c) * 256 + (((4 * kk + j) ^ c) << 4)); };
+  u32x4 qb[kQueryInLds ? 1 : NC][4];
+  float qsum_[kQueryInLds ? 1 : NC][NG], kappa_[kQueryInLds ? 1 : NC];       // (more than one column set: read where they are used)
 #pragma unroll
   for (int cs = 0; cs < NC; ++cs) {
-    const int r = 16 * cs + c;
+    if constexpr (!kQueryInLds) {
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) qb[cs][kk] = *reinterpret_cast<const u32x4*>(sm + r * 256 + (((4 * kk + j) ^ (r & 15)) << 4));
-    const float4v q4 = *reinterpret_cast<const float4v*>(sm_sums[r]);
+      for (int kk = 0; kk < 4; ++kk) qb[cs][kk] = query_operand(cs, kk);
 #pragma unroll
-    for (int n = 0; n < NG; ++n) qsum[cs][n] = q4[n];
-    kappa[cs] = sm_kappa[r];
-    my_p[cs] = p0 + min(row0 + r, rows - 1) / R;
+      for (int n = 0; n < NG; ++n) qsum_[cs][n] = sm_sums[16 * cs + c][n] * kUnitK;
+      kappa_[cs] = sm_kappa[16 * cs + c] * (1.0f / kUnitK);
+    }
   }
-  __syncthreads();                                         // (the query's place is the wavefronts' from here on)
+  auto query_sum = [&](int cs, int n) {                    // (scores carry the codes' unit)
+    if constexpr (kQueryInLds) return sm_sums[16 * cs + c][n] * kUnitK; else return qsum_[cs][n];
+  };
+  auto kappa = [&](int cs) { if constexpr (kQueryInLds) return sm_kappa[16 * cs + c] * (1.0f / kUnitK); else return kappa_[cs]; };
   uint8_t* const st = sm + wave * kWaveBytes;
-  uint8_t* const st_meta = st + NK * 1024;
+  uint8_t* const st_v = st + 512 * BK;
+  uint8_t* const st_meta = st_v + 512 * BV;
 
   // value scales of 64 and more take their bits of room from the weights
-  const int scale_exp = RAWV ? 0 : a.cache.v_scale_exp[(int64_t)b * g.kv_heads + h];
   const float weight_bits = kFewWeightBits - (float)max(scale_exp - 20, 0);
   const int sw = key_swizzle<BK>(c);
+  // where the scales and zeros of part n (of NG) of a row lie: group n >> shift of the tensor's
+  const int ngk = RAWK ? 1 : g.ng_k, ngv = RAWV ? 1 : g.ng_v;
+  const int shift_k = NG == ngk ? 0 : NG == 2 * ngk ? 1 : 2, shift_v = NG == ngv ? 0 : NG == 2 * ngv ? 1 : 2;
+  auto meta_k = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + ((x4 * ngk + (n >> shift_k)) * 16 + 4 * j) * 4); };
+  auto meta_v = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + 16 * nmk + ((x4 * ngv + (n >> shift_v)) * 16 + 4 * j) * 4); };
 
   float4v acc[NC][8];
   float m[NC], l[NC], zacc[NC][NG];
@@ -215,25 +252,36 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
     for (int n = 0; n < NG; ++n) zacc[cs][n] = 0.0f;
   }
 
-  // where the scales and zeros of part n (of NG) of a row lie: group n >> shift of the tensor's
-  const int ngk = RAWK ? 1 : g.ng_k, ngv = RAWV ? 1 : g.ng_v;
-  const int shift_k = NG == ngk ? 0 : NG == 2 * ngk ? 1 : 2, shift_v = NG == ngv ? 0 : NG == 2 * ngv ? 1 : 2;
-  auto meta_k = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + ((x4 * ngk + (n >> shift_k)) * 16 + 4 * j) * 4); };
-  auto meta_v = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + 16 * nmk + ((x4 * ngv + (n >> shift_v)) * 16 + 4 * j) * 4); };
-  auto compute = [&](Step<BK, BV>& s, int blk) {
-    const int t0 = 32 * blk;
-    // keys and scales through LDS
+  for (int x = x0; x < end; x += NW) {
+    const int t0 = 32 * block_at(x);
+    const bool tail = t0 + 32 > limit;
+    // ---- the block to LDS, the next one under way
 #pragma unroll
-    for (int i = 0; i < NK; ++i) *reinterpret_cast<u32x4*>(st + 1024 * i + 16 * lane) = s.k[i];
-    if constexpr (!RAWK || !RAWV) *reinterpret_cast<u32x4*>(st_meta + 16 * lane) = s.meta;
+    for (int i = 0; i < NK; ++i)
+      if (64 * (i + 1) <= 32 * BK || lane < 32 * BK - 64 * i) *reinterpret_cast<u32x4*>(st + 1024 * i + 16 * lane) = step.k[i];
+    store_value_piece<BV>(step.v, st_v, lane);
+    if constexpr (!RAWK || !RAWV) {
+      if (tail) {                                          // (the sequence's last block: what lies behind its end is no number)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) step.meta[r] = t0 + meta_token + r < limit ? step.meta[r] : 0u;
+      }
+      *reinterpret_cast<u32x4*>(st_meta + 16 * lane) = step.meta;
+    }
+    {
+      const bool more = x + NW < end;                      // uniform
+      load(step, block_at(more ? x + NW : x), more ? page : 0, more ? ~0u : 0u);
+      page = x + 2 * NW < end ? page_of(block_at(x + 2 * NW)) : 0;
+    }
     __builtin_amdgcn_wave_barrier();
+
+    // ---- scores
     float sc[NC][8];
 #pragma unroll
     for (int x4 = 0; x4 < 2; ++x4) {
+      constexpr int NGK = RAWK ? 1 : NG;
       u32x4 ka[4];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) ka[kk] = key_operand<BK>(st, 16 * x4 + c, sw, kk, j, raw_bf);
-      constexpr int NGK = RAWK ? 1 : NG;
 #pragma unroll
       for (int cs = 0; cs < NC; ++cs)
 #pragma unroll
@@ -245,12 +293,13 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
 #pragma unroll
         for (int cs = 0; cs < NC; ++cs) {
           float4v d = float4v{0.f, 0.f, 0.f, 0.f};
+          const float qs = RAWK ? 0.0f : query_sum(cs, n);
 #pragma unroll
-          for (int kk = n * (4 / NGK); kk < (n + 1) * (4 / NGK); ++kk) d = mma16(ka[kk], qb[cs][kk], d);
+          for (int kk = n * (4 / NGK); kk < (n + 1) * (4 / NGK); ++kk) d = mma16(ka[kk], kQueryInLds ? query_operand(cs, kk) : qb[kQueryInLds ? 0 : cs][kk], d);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float& y = sc[cs][4 * x4 + r];
-            y = RAWK ? d[r] : fmaf(meta_s(mk[r]), d[r], fmaf(meta_z(mk[r]), qsum[cs][n], y));
+            y = RAWK ? d[r] : fmaf(meta_s(mk[r]), d[r], fmaf(meta_z(mk[r]), qs, y));
           }
         }
       }
@@ -260,24 +309,25 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
     if (!whole) {
 #pragma unroll
       for (int cs = 0; cs < NC; ++cs) {
-        const int my_lo = a.window ? my_p[cs] - a.window : -1;
+        const int my_p = sm_pos[16 * cs + c], my_lo = a.window ? my_p - a.window : -1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int t = t0 + 16 * (i >> 2) + 4 * j + (i & 3);
-          const bool seen = (t <= my_p[cs]) & ((t > my_lo) | (t < a.sinks));
+          const bool seen = (t <= my_p) & ((t > my_lo) | (t < a.sinks));
           sc[cs][i] = seen ? sc[cs][i] : -INFINITY;
         }
       }
     }
-    float p[NC][8];
+    // ---- weights
 #pragma unroll
     for (int cs = 0; cs < NC; ++cs) {
+      const float kap = kappa(cs);
       float most = sc[cs][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) most = fmaxf(most, sc[cs][i]);
-      most *= kappa[cs];
+      most *= kap;
       if (__any(most > m[cs] + kFewSlack)) {
-        const float m_new = fmaxf(m[cs], over_rows_max(most)), f = exp2f(m[cs] - m_new);
+        const float m_new = fmaxf(m[cs], over_rows_max(most)), f = __builtin_amdgcn_exp2f(m[cs] - m_new);
         m[cs] = m_new;
         l[cs] *= f;
 #pragma unroll
@@ -287,120 +337,65 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
       }
       const float off = weight_bits - m[cs];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { p[cs][i] = __builtin_amdgcn_exp2f(fmaf(sc[cs][i], kappa[cs], off)); l[cs] += p[cs][i]; }
+      for (int i = 0; i < 8; ++i) { sc[cs][i] = __builtin_amdgcn_exp2f(fmaf(sc[cs][i], kap, off)); l[cs] += sc[cs][i]; }
     }
-    const bool tail = t0 + 32 > limit;
-    const int valid = limit - (t0 + 4 * j);                // tokens 16 x4 + r of this lane below it exist
-    // weights of every part of the value rows (8 / NGV channel tiles each), and the product with its tiles
+    // ---- weights of every part of the value rows (8 / NGV channel tiles each), and the product with its tiles
     constexpr int NGV = RAWV ? 1 : NG;
+    const int valid = limit - (t0 + 4 * j);                // tokens 16 x4 + r of this lane below it exist
+    uint32_t vw[2 * BV];
+    read_value_piece<BV>(vw, st_v, lane);
 #pragma unroll
     for (int n = 0; n < NGV; ++n) {
-      u32x4 mv[2], hi[NC], lo[NC];
-      if constexpr (!RAWV) {
-#pragma unroll
-        for (int x4 = 0; x4 < 2; ++x4) {
-          mv[x4] = meta_v(x4, n);
-          if (tail) {                                      // (what lies behind the sequence's end is no number)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) mv[x4][r] = 16 * x4 + r < valid ? mv[x4][r] : 0u;
-          }
-        }
-      }
+      u32x4 mv[2], hi[NC], lo2[NC];
+      if constexpr (!RAWV) { mv[0] = meta_v(0, n); mv[1] = meta_v(1, n); }
 #pragma unroll
       for (int cs = 0; cs < NC; ++cs) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float w0 = p[cs][2 * i], w1 = p[cs][2 * i + 1];
+          float w0 = sc[cs][2 * i], w1 = sc[cs][2 * i + 1];
+          half2v y;
           if constexpr (!RAWV) {
             const uint32_t e0 = mv[i >> 1][2 * (i & 1)], e1 = mv[i >> 1][2 * (i & 1) + 1];
             zacc[cs][n] = fmaf(w0, meta_z(e0), zacc[cs][n]);
             zacc[cs][n] = fmaf(w1, meta_z(e1), zacc[cs][n]);
-            w0 *= meta_s(e0);
-            w1 *= meta_s(e1);
+            if constexpr (FINE) { w0 *= meta_s(e0); w1 *= meta_s(e1); }
+            else {                                         // (product and rounding in one instruction each)
+              y[0] = (_Float16)fmaf(w0, meta_s(e0), 0.0f);
+              y[1] = (_Float16)fmaf(w1, meta_s(e1), 0.0f);
+            }
           }
-          half2v x;
-          x[0] = (_Float16)w0; x[1] = (_Float16)w1;
-          hi[cs][i] = as_u32(x);
+          if constexpr (RAWV || FINE) { y[0] = (_Float16)w0; y[1] = (_Float16)w1; }
+          hi[cs][i] = as_u32(y);
           if constexpr (FINE) {
-            half2v y;
-            y[0] = (_Float16)(w0 - (float)x[0]); y[1] = (_Float16)(w1 - (float)x[1]);
-            lo[cs][i] = as_u32(y);
+            half2v z;
+            z[0] = (_Float16)(w0 - (float)y[0]); z[1] = (_Float16)(w1 - (float)y[1]);
+            lo2[cs][i] = as_u32(z);
           }
         }
       }
 #pragma unroll
       for (int dt = n * (8 / NGV); dt < (n + 1) * (8 / NGV); ++dt) {
-        u32x4 va = value_operand<BV>(s.v, dt);
+        u32x4 va = value_operand<BV>(vw, dt);
         if constexpr (RAWV) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint32_t x = raw_to_half2(va[i], raw_bf);
+            uint32_t y = raw_to_half2(va[i], raw_bf);
             const int at = 16 * (i >> 1) + 2 * (i & 1);
-            if (tail) x &= (at < valid ? 0x0000FFFFu : 0u) | (at + 1 < valid ? 0xFFFF0000u : 0u);
-            va[i] = x;
+            if (tail) y &= (at < valid ? 0x0000FFFFu : 0u) | (at + 1 < valid ? 0xFFFF0000u : 0u);
+            va[i] = y;
           }
         }
 #pragma unroll
         for (int cs = 0; cs < NC; ++cs) {
           acc[cs][dt] = mma16(va, hi[cs], acc[cs][dt]);
-          if constexpr (FINE) acc[cs][dt] = mma16(va, lo[cs], acc[cs][dt]);
+          if constexpr (FINE) acc[cs][dt] = mma16(va, lo2[cs], acc[cs][dt]);
         }
       }
     }
     __builtin_amdgcn_wave_barrier();
-  };
-
-  for (int i0 = 0; i0 < n_my; i0 += ST) {
-#pragma unroll
-    for (int s = 0; s < ST; ++s) {
-      const int i = i0 + s;
-      if (i >= n_my) break;                                // uniform
-      const int next = i + ST < n_my ? i + ST : 0;
-      const int page = page_of(block_of(next));
-      compute(ring[s], block_of(i));
-      load(ring[s], block_of(next), page, i + ST < n_my ? ~0u : 0u);
-    }
   }
 
-  // ---- join the wavefronts, halves onto halves
-  constexpr int kJoin = NC * 64 * (32 + 6) * 4;            // bytes of one wavefront's sums
-  __syncthreads();
-#pragma unroll
-  for (int half = NW / 2; half >= 1; half >>= 1) {
-    if (wave >= half && wave < 2 * half) {
-      float* to = reinterpret_cast<float*>(sm + (wave - half) * kJoin);
-#pragma unroll
-      for (int cs = 0; cs < NC; ++cs) {
-        float* q = to + cs * (64 * 38);
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<float4v*>(q + 256 * dt + 4 * lane) = acc[cs][dt];
-        *reinterpret_cast<float4v*>(q + 2048 + 4 * lane) = float4v{zacc[cs][0], zacc[cs][NG > 1], zacc[cs][NG > 2 ? 2 : 0], zacc[cs][NG > 2 ? 3 : 0]};
-        q[2304 + lane] = m[cs];
-        q[2368 + lane] = l[cs];
-      }
-    }
-    __syncthreads();
-    if (wave < half) {
-      const float* from = reinterpret_cast<const float*>(sm + wave * kJoin);
-#pragma unroll
-      for (int cs = 0; cs < NC; ++cs) {
-        const float* q = from + cs * (64 * 38);
-        const float m2 = q[2304 + lane], l2 = q[2368 + lane];
-        const float m_new = fmaxf(m[cs], m2), f = exp2f(m[cs] - m_new), f2 = exp2f(m2 - m_new);
-        m[cs] = m_new;
-        l[cs] = l[cs] * f + l2 * f2;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) acc[cs][dt] = acc[cs][dt] * f + *reinterpret_cast<const float4v*>(q + 256 * dt + 4 * lane) * f2;
-        const float4v z = *reinterpret_cast<const float4v*>(q + 2048 + 4 * lane);
-#pragma unroll
-        for (int n = 0; n < NG; ++n) zacc[cs][n] = zacc[cs][n] * f + z[n] * f2;
-      }
-    }
-    __syncthreads();
-  }
-  if (wave != 0) return;
-
-  // ---- results: acc[cs][dt][r] is channel 16 dt + 4 j + r of row 16 cs + c
+  // ---- join the wavefronts: everybody's maxima and weight sums, then sums of channels rescaled to the common maximum
 #pragma unroll
   for (int cs = 0; cs < NC; ++cs) {
     l[cs] = over_rows_sum(l[cs]);
@@ -408,28 +403,26 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
     for (int n = 0; n < NG; ++n) zacc[cs][n] = over_rows_sum(zacc[cs][n]);
     if constexpr (!RAWV) {
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        acc[cs][dt] += zacc[cs][dt * NG / 8];
-      }
+      for (int dt = 0; dt < 8; ++dt) acc[cs][dt] = acc[cs][dt] * (1.0f / kUnitV) + zacc[cs][dt * NG / 8];
       if (g.rotate_v) {                                    // back to the input basis (linear, so sums of parts as well)
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
-          float4v& x = acc[cs][dt];
-          x = float4v{x[0] + x[1], x[0] - x[1], x[2] + x[3], x[2] - x[3]};
-          x = float4v{x[0] + x[2], x[1] + x[3], x[0] - x[2], x[1] - x[3]};
+          float4v& y = acc[cs][dt];
+          y = float4v{y[0] + y[1], y[0] - y[1], y[2] + y[3], y[2] - y[3]};
+          y = float4v{y[0] + y[2], y[1] + y[3], y[0] - y[2], y[1] - y[3]};
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            float o = __shfl_xor(x[r], 16);
-            x[r] = j & 1 ? o - x[r] : x[r] + o;
-            o = __shfl_xor(x[r], 32);
-            x[r] = j & 2 ? o - x[r] : x[r] + o;
+            float o = __shfl_xor(y[r], 16);
+            y[r] = j & 1 ? o - y[r] : y[r] + o;
+            o = __shfl_xor(y[r], 32);
+            y[r] = j & 2 ? o - y[r] : y[r] + o;
           }
         }
 #pragma unroll
-        for (int step = 1; step < 8; step <<= 1)
+        for (int half = 1; half < 8; half <<= 1)
 #pragma unroll
           for (int dt = 0; dt < 8; ++dt)
-            if (!(dt & step)) { const float4v u = acc[cs][dt], w = acc[cs][dt + step]; acc[cs][dt] = u + w; acc[cs][dt + step] = u - w; }
+            if (!(dt & half)) { const float4v u = acc[cs][dt], w = acc[cs][dt + half]; acc[cs][dt] = u + w; acc[cs][dt + half] = u - w; }
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
@@ -439,21 +432,54 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
           }
       }
     }
-    const int row = row0 + 16 * cs + c;
-    if (row < rows) {
-      const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
-      if (a.splits > 1) {
-        float* rec = a.ws + (hq * a.splits + split) * kRec;
+    if (j == 0) { sm_m[wave][16 * cs + c] = m[cs]; sm_l[wave][16 * cs + c] = l[cs]; }
+  }
+  __syncthreads();
+  constexpr int kParts = few_join_parts<NC>(), kWidth = kHeadDim / kParts, kStride = kWidth + 4;
+  float* const sums = reinterpret_cast<float*>(sm);
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<float4v*>(rec + 16 * dt + 4 * j) = acc[cs][dt];
-        if (j == 0) { rec[kHeadDim] = m[cs]; rec[kHeadDim + 1] = l[cs]; }
-      } else {
-        const float inv = l[cs] > 0.0f ? 1.0f / l[cs] : 0.0f;              // (a row that sees nothing: zeros)
+  for (int part = 0; part < kParts; ++part) {
+    if (part) __syncthreads();
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          const float4v x = acc[cs][dt] * inv;
-          const float y[4] = {x[0], x[1], x[2], x[3]};
-          store_out4(a.out, a.out_dtype, hq * kHeadDim + 16 * dt + 4 * j, y);
+    for (int cs = 0; cs < NC; ++cs) {
+      float top = sm_m[0][16 * cs + c];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][16 * cs + c]);
+      const float f = __builtin_amdgcn_exp2f(m[cs] - top);
+#pragma unroll
+      for (int dt = part * (8 / kParts); dt < (part + 1) * (8 / kParts); ++dt)
+        *reinterpret_cast<float4v*>(sums + (wave * (16 * NC) + 16 * cs + c) * kStride + 16 * dt + 4 * j - part * kWidth) = acc[cs][dt] * f;
+    }
+    __syncthreads();
+    // 8 channels a thread, 16 (kParts = 2: 8) threads a row
+    constexpr int kThreads = kWidth / 8;
+    for (int r = tid / kThreads; r < 16 * NC; r += 64 * NW / kThreads) {
+      const int d0 = 8 * (tid % kThreads), row = row0 + r;
+      float top = sm_m[0][r], total = 0.0f;
+#pragma unroll
+      for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][r]);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) total += sm_l[w][r] * __builtin_amdgcn_exp2f(sm_m[w][r] - top);
+      float4v y0 = float4v{0.f, 0.f, 0.f, 0.f}, y1 = y0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float* from = sums + (w * (16 * NC) + r) * kStride + d0;
+        y0 += *reinterpret_cast<const float4v*>(from);
+        y1 += *reinterpret_cast<const float4v*>(from + 4);
+      }
+      if (row < rows) {
+        const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
+        const int d = part * kWidth + d0;
+        if (a.splits > 1) {
+          float* rec = a.ws + (hq * a.splits + split) * kRec;
+          *reinterpret_cast<float4v*>(rec + d) = y0;
+          *reinterpret_cast<float4v*>(rec + d + 4) = y1;
+          if (d == 0) { rec[kHeadDim] = top; rec[kHeadDim + 1] = total; }
+        } else {
+          const float inv = total > 0.0f ? 1.0f / total : 0.0f;              // (a row that sees nothing: zeros)
+          const float z0[4] = {y0[0] * inv, y0[1] * inv, y0[2] * inv, y0[3] * inv}, z1[4] = {y1[0] * inv, y1[1] * inv, y1[2] * inv, y1[3] * inv};
+          store_out4(a.out, a.out_dtype, hq * kHeadDim + d, z0);
+          store_out4(a.out, a.out_dtype, hq * kHeadDim + d + 4, z1);
         }
       }
     }
@@ -463,17 +489,17 @@ __global__ __launch_bounds__((64 * few_waves<BK, BV, NC>()), 2) void few_kernel(
 }  // namespace
 
 template <int BK, int BV, int NC, int NG> hipError_t launch_few_groups(const ChunkArgs& a, hipStream_t stream) {
-  const dim3 grid(a.g.batch * a.g.kv_heads, a.splits, (a.n_q * a.heads_per_kv + 16 * NC - 1) / (16 * NC)), block(64 * few_waves<BK, BV, NC>());
+  const dim3 grid(a.g.batch * a.g.kv_heads, a.splits, (a.n_q * a.heads_per_kv + 16 * NC - 1) / (16 * NC)), block(64 * kFewWaves);
   if (a.out_dtype == KVQ_F32) hipLaunchKernelGGL((few_kernel<BK, BV, NC, NG, true>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL((few_kernel<BK, BV, NC, NG, false>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 template <int BK, int BV, int NC> hipError_t launch_few_pair(const ChunkArgs& a, hipStream_t stream) {
   const int ngk = BK == 16 ? 1 : a.g.ng_k, ngv = BV == 16 ? 1 : a.g.ng_v, ng = ngk > ngv ? ngk : ngv;
-  if (ng == 1) return launch_few_groups<BK, BV, NC, 1>(a, stream);
+  if constexpr (NC <= few_max_sets(BK, BV, 1)) if (ng == 1) return launch_few_groups<BK, BV, NC, 1>(a, stream);
   if constexpr (BK != 16 || BV != 16) {
-    if (ng == 2) return launch_few_groups<BK, BV, NC, 2>(a, stream);
-    if (ng == 4) return launch_few_groups<BK, BV, NC, 4>(a, stream);
+    if constexpr (NC <= few_max_sets(BK, BV, 2)) if (ng == 2) return launch_few_groups<BK, BV, NC, 2>(a, stream);
+    if constexpr (NC <= few_max_sets(BK, BV, 4)) if (ng == 4) return launch_few_groups<BK, BV, NC, 4>(a, stream);
   }
   return hipErrorInvalidValue;
 }
@@ -481,7 +507,12 @@ template <int BK, int BV, int NC> hipError_t launch_few_pair(const ChunkArgs& a,
 #define KVQ_PAIR(k, v) KVQ_PAIR_(k, v)
 #define KVQ_PAIR_(k, v) launch_few_k##k##v##v
 hipError_t KVQ_PAIR(KVQ_INST_BK, KVQ_INST_BV)(const ChunkArgs& a, int sets, hipStream_t stream) {
-  return sets == 1 ? launch_few_pair<KVQ_INST_BK, KVQ_INST_BV, 1>(a, stream) : launch_few_pair<KVQ_INST_BK, KVQ_INST_BV, 2>(a, stream);
+  switch (sets) {
+    case 1: return launch_few_pair<KVQ_INST_BK, KVQ_INST_BV, 1>(a, stream);
+    case 2: return launch_few_pair<KVQ_INST_BK, KVQ_INST_BV, 2>(a, stream);
+    case 3: return launch_few_pair<KVQ_INST_BK, KVQ_INST_BV, 3>(a, stream);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace kvq
