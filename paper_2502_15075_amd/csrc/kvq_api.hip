@@ -361,9 +361,11 @@ kvq_status chunk_common(const kvq_layout* layout, const kvq_cache* cache, const 
   const kvq::ChunkPlan plan = kvq::plan_chunk(a.g, a.heads_per_kv, n_q, max_seq_len, window, sinks);
   a.splits = plan.splits;
   const size_t record = kvq::chunk_record_bytes(layout->batch, n_q, q_heads, 2) / 2;
-  const size_t room = workspace ? workspace_bytes / record : 0;
+  const size_t counters = kvq::chunk_counter_bytes(a.g, a.heads_per_kv, n_q);
+  const size_t room = workspace && workspace_bytes > counters ? (workspace_bytes - counters) / record : 0;
   if ((size_t)a.splits > room) a.splits = room < 2 ? 1 : (int32_t)room;
-  return kvq::launch_chunk_attention(a, plan.few_sets, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+  a.words = (kvq::MergeWord*)((char*)workspace + record * a.splits);
+  return kvq::launch_chunk_attention(a, plan, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 }  // namespace
 
@@ -372,9 +374,12 @@ kvq_status kvq_chunk_workspace_bytes(const kvq_layout* layout, int32_t q_heads, 
   kvq_status st = chunk_check(layout, q_heads, n_q, max_seq_len, window, sinks);
   if (st != KVQ_OK) return st;
   if (!bytes_out) return KVQ_ERR_INVALID_ARG;
+  *bytes_out = 0;
+  if (n_q == 0) return KVQ_OK;
   const kvq::Geom g = kvq::make_geom(*layout);
-  *bytes_out = n_q == 0 ? 0 : kvq::chunk_record_bytes(layout->batch, n_q, q_heads,
-                                                      kvq::plan_chunk(g, q_heads / layout->kv_heads, n_q, max_seq_len, window, sinks).splits);
+  const int heads = q_heads / layout->kv_heads;
+  const size_t records = kvq::chunk_record_bytes(layout->batch, n_q, q_heads, kvq::plan_chunk(g, heads, n_q, max_seq_len, window, sinks).splits);
+  if (records) *bytes_out = records + kvq::chunk_counter_bytes(g, heads, n_q);
   return KVQ_OK;
 }
 

@@ -19,6 +19,9 @@ constexpr int kRec = kHeadDim + 4;       // floats of a partial record: 128 sums
 
 __device__ __forceinline__ half2v as_half2(uint32_t x) { return __builtin_bit_cast(half2v, x); }
 __device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast(uint32_t, x); }
+// A binary32 value whose two binary16 parts are formed next.  Left to itself the compiler merges the operation that made it with the rounding
+// of the first part (one rounding instead of two, the other side of a tie), but not with the difference that becomes the second.
+__device__ __forceinline__ float as_rounded(float x) { asm("" : "+v"(x)); return x; }
 __device__ __forceinline__ float other_half(float x) {           // lane ^ 32's value
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
@@ -49,7 +52,7 @@ __device__ __forceinline__ int key_fields(int bits) { return bits == 3 ? 8 : bit
 
 // Query rows [row0, row0 + n) of a kv head (row = query token * heads_per_kv + head; rows behind the last repeat it) to LDS, by 16 lanes a
 // row: binary16 in slot order, 256 bytes a row whose 16-byte pieces are permuted by the row's number (piece p at p ^ (r & 15)); the sums of
-// ng equal parts of the row (4 at most), each as two binary16 parts (`parts`, may be null) or in binary32 (`sums`, may be null); and the factor of the row's scores.
+// ng equal parts of the row (4 at most), each as two binary16 parts (`parts`, may be null) or in binary32 (`sums`, may be null); and the factor of the row's scores (every row is scaled by a power of two).
 template <int THREADS>
 __device__ __forceinline__ void stage_query(const ChunkArgs& a, int b, int h, int row0, int rows, int n, int ng, uint8_t* dst, uint32_t (*parts)[4],
                                             float (*sums)[4], float* kappa) {
@@ -78,19 +81,24 @@ __device__ __forceinline__ void stage_query(const ChunkArgs& a, int b, int h, in
     sum += lane_xor<2>(sum);
     if (ng <= 2) sum += lane_xor<4>(sum);
     if (ng == 1) sum += lane_xor<8>(sum);
-    // a row whose sums do not fit binary16 is scaled down by a power of two as a whole
+    // Every row is scaled by a power of two that takes its largest element or sum to [2^13, 2^14): sums then fit binary16, and no element that
+    // counts is a subnormal (next to codes that are, the matrix unit loses those).  Elements below 2^-27 of the largest lose bits.
     float most = fabsf(sum);
-    if (ng == 4) most = fmaxf(most, lane_xor<4>(most));
-    if (ng >= 2) most = fmaxf(most, lane_xor<8>(most));
-    const int down = max((int)((__float_as_uint(most) >> 23) & 0xFF) - (127 + 14), 0);
-    const float unit = __uint_as_float((uint32_t)(127 - down) << 23);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+    most = fmaxf(most, lane_xor<1>(most));
+    most = fmaxf(most, lane_xor<2>(most));
+    most = fmaxf(most, lane_xor<4>(most));
+    most = fmaxf(most, lane_xor<8>(most));
+    const int up = 127 + 13 - max((int)(__float_as_uint(most) >> 23), 90);   // (rows of zeros: any factor will do)
+    const float unit = __uint_as_float((uint32_t)(127 + up) << 23);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int slot = (d0 & ~31) + key_slot((d0 & 31) + e, fields);
       const int at = (((slot >> 3) ^ (r & 15)) << 4) + (slot & 7) * 2;
       *reinterpret_cast<_Float16*>(dst + r * 256 + at) = (_Float16)(x[e] * unit);
     }
-    if (lane16 == 0) kappa[r] = a.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 + down) << 23);
+    if (lane16 == 0) kappa[r] = a.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 - up) << 23);
     const int q = lane16 >> 2;                         // part q's sum: in lane 16 q / ng of the row (all lanes take part)
     const float group_sum = __shfl(sum, (lane & ~15) + (ng == 1 ? 0 : ng == 2 ? 8 * (q & 1) : 4 * q));
     if ((lane16 & 3) == 0) {
@@ -117,6 +125,78 @@ __device__ __forceinline__ void store_out4(void* out, int out_dtype, int64_t o, 
       w = make_uint2(f32_to_bf16_bits(y[0]) | (uint32_t)f32_to_bf16_bits(y[1]) << 16, f32_to_bf16_bits(y[2]) | (uint32_t)f32_to_bf16_bits(y[3]) << 16);
     }
     *reinterpret_cast<uint2*>((uint16_t*)out + o) = w;
+  }
+}
+
+// ---- partial records: [row][split][kRec], a row's 128 sums, its maximum and its weight sum.  They travel between workgroups that may sit on
+// different parts of the chip, so stores and loads are device-scope atomic accesses, two floats each.
+__device__ __forceinline__ void store_record2(float* p, float x, float y) {
+  const uint64_t w = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_record2(const float* p) {
+  const uint64_t w = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+}
+// The rules of kvq_merge_count.h.  One thread calls merge_announce before its workgroup stores records; all threads call merge_arrive behind
+// their stores: true (in all of them) in the workgroup that brings the count to `records`.
+__device__ __forceinline__ void merge_announce(MergeWord* word, MergeWord tag) {
+  (void)__hip_atomic_fetch_max(word, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool merge_arrive(MergeWord* word, MergeWord tag, int records, int tid, int* flag) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");   // (keeps the compiler from moving a store behind the wait)
+  __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wavefront's record stores are performed
+  __syncthreads();                                         // (and so are the other wavefronts')
+  if (tid == 0) {
+    MergeWord before = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (merge_unmarked(before, tag)) {                     // (rare; a swap fails only because another workgroup got on)
+      MergeWord seen = before + 1;
+      while (merge_unmarked(seen, tag) &&
+             !__hip_atomic_compare_exchange_strong(word, &seen, tag | 1ull, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) {}
+      before = merge_unmarked(seen, tag) ? tag : __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    const bool last = merge_last(before, records);
+    if (last) __hip_atomic_store(word, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag;
+}
+// Rows [row0, row0 + n) of a kv head from their records: 32 threads a row, four channels each, four records at a time under a running maximum.
+template <int THREADS>
+__device__ __forceinline__ void merge_rows(const ChunkArgs& a, int b, int h, int row0, int n, int tid) {
+  const int R = a.heads_per_kv;
+  for (int idx = tid; idx < 32 * n; idx += THREADS) {
+    const int row = row0 + (idx >> 5), d = 4 * (idx & 31);
+    const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
+    const float* rec = a.ws + hq * a.splits * kRec;
+    float m = kNoMax, l = 0.0f, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+      float2 ml[4], u[4], v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float* r = rec + min(s0 + k, a.splits - 1) * kRec;
+        ml[k] = load_record2(r + kHeadDim); u[k] = load_record2(r + d); v[k] = load_record2(r + d + 2);
+      }
+      float top = m;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = s0 + k < a.splits ? fmaxf(top, ml[k].x) : top;
+      const float f0 = __builtin_amdgcn_exp2f(m - top);
+      l *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= f0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = s0 + k < a.splits ? __builtin_amdgcn_exp2f(ml[k].x - top) : 0.0f;
+        l = fmaf(f, ml[k].y, l);
+        y[0] = fmaf(f, u[k].x, y[0]); y[1] = fmaf(f, u[k].y, y[1]); y[2] = fmaf(f, v[k].x, y[2]); y[3] = fmaf(f, v[k].y, y[3]);
+      }
+      m = top;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;          // (a row that sees nothing: zeros)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] *= inv;
+    store_out4(a.out, a.out_dtype, hq * kHeadDim + d, y);
   }
 }
 

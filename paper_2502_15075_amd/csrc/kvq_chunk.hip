@@ -11,7 +11,8 @@
 // operand's order.
 //
 // A tile of 64 tokens is unpacked once per workgroup into LDS: keys as binary16 codes (0 .. 255: exact, so their products with the
-// query are too), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are rounded alike).  Key scales
+// query are too), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are rounded alike).  For outputs in
+// binary32 (FINE) weights and values travel as two binary16 parts each, 2^-22 of them, and three products are summed.  Key scales
 // are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the query's
 // group sums, each split into two binary16 parts.
 #include "kvq_attend.h"
@@ -94,15 +95,17 @@ __device__ __forceinline__ Walk make_walk(int p_first, int p_last, int window, i
   return w;
 }
 
-template <int NG>
+template <int NG, bool FINE>
 __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t sm_tile[2 * kTileTokens * kHeadDim * 2];   // keys, then values
+  constexpr int kTileBytes = kTileTokens * kHeadDim * 2;
+  __shared__ __attribute__((aligned(16))) uint8_t sm_tile[(FINE ? 3 : 2) * kTileBytes];      // keys, values, the values' second parts
   __shared__ __attribute__((aligned(16))) float sm_scale[4][kTileTokens];                      // key scales, by matrix row
   __shared__ __attribute__((aligned(16))) uint32_t sm_zero[kTileTokens][4];                    // key zeros, each twice
   __shared__ __attribute__((aligned(16))) uint32_t sm_qsum[kTileRows][4];                      // group sums of the query, two parts each
   __shared__ float sm_kappa[kTileRows];
+  __shared__ int sm_last;
   uint8_t* const sm_k = sm_tile;
-  uint8_t* const sm_v = sm_tile + kTileTokens * kHeadDim * 2;
+  uint8_t* const sm_v = sm_tile + kTileBytes;
 
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -151,6 +154,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
   float m = kNoMax, l = 0.0f;
+  const bool two_parts = g.bits_v != 16;                   // (patterns of an unquantized plane have no second part)
   const uint32_t one_k = one_k_pattern(), v_mask = ((1u << min(g.bits_v, 15)) - 1u) * 0x00010001u;
 
   for (int ti = t_begin; ti < t_end; ++ti) {
@@ -223,6 +227,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int dt = 4 * half + t;
+          u32x4 second;
           if (t == 0 || (t == 2 && per_group == 2)) {
             const int gr = dt / per_group;
             const uint32_t* mp = (const uint32_t*)a.cache.v_meta + meta_index(base + 32 * sblk, gr, g.ng_v) + 4 * j;
@@ -238,8 +243,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
           for (int v = 0; v < 4; ++v) {
             const uint32_t e0 = m4[v >> 1][2 * (v & 1)], e1 = m4[v >> 1][2 * (v & 1) + 1];
             const half2v s = as_half2((e0 & 0xFFFFu) | (e1 << 16)), z = as_half2((e0 >> 16) | (e1 & 0xFFFF0000u));
-            f[4 * t + v] = as_u32(__builtin_elementwise_fma(whole_to_half2(f[4 * t + v], v_mask, one_k), s, z));
+            const half2v code = whole_to_half2(f[4 * t + v], v_mask, one_k);
+            if constexpr (FINE) {
+              const float x = as_rounded(fmaf((float)code[0], (float)s[0], (float)z[0])), y = as_rounded(fmaf((float)code[1], (float)s[1], (float)z[1]));
+              half2v hi, lo;
+              hi[0] = (_Float16)x; hi[1] = (_Float16)y;
+              lo[0] = (_Float16)(x - (float)hi[0]); lo[1] = (_Float16)(y - (float)hi[1]);
+              f[4 * t + v] = as_u32(hi);
+              second[v] = as_u32(lo);
+            } else {
+              f[4 * t + v] = as_u32(__builtin_elementwise_fma(code, s, z));
+            }
           }
+          if constexpr (FINE) *reinterpret_cast<u32x4*>(sm_v + kTileBytes + blk * 8192 + (j * 128 + 16 * dt + dl) * 16) = second;
         }
       }
 #pragma unroll
@@ -299,21 +315,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
           for (int i = 0; i < 16; ++i) acc[ct][i] *= f;
       }
       const float off = kWeightBits - m;
-      u32x4 pw[2];
+      u32x4 pw[2], pl[2];
 #pragma unroll
       for (int v = 0; v < 8; ++v) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * v], kappa, off)), y = __builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], kappa, off));
         half2v p;
-        p[0] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * v], kappa, off));
-        p[1] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], kappa, off));
-        l = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, l, false);
+        p[0] = (_Float16)x;
+        p[1] = (_Float16)y;
         pw[v >> 2][v & 3] = as_u32(p);
+        if constexpr (FINE) {
+          l += x + y;
+          half2v q;
+          q[0] = (_Float16)(x - (float)p[0]); q[1] = (_Float16)(y - (float)p[1]);
+          pl[v >> 2][v & 3] = as_u32(q);
+        } else {
+          l = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, l, false);
+        }
       }
       const uint8_t* vt = sm_v + blk * 8192;
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-          acc[ct] = mma32(*reinterpret_cast<const u32x4*>(vt + ((2 * st + hh) * 128 + 32 * ct + col) * 16), pw[st], acc[ct]);
+        for (int ct = 0; ct < 4; ++ct) {
+          const int at = ((2 * st + hh) * 128 + 32 * ct + col) * 16;
+          const u32x4 va = *reinterpret_cast<const u32x4*>(vt + at);
+          acc[ct] = mma32(va, pw[st], acc[ct]);
+          if constexpr (FINE) {
+            acc[ct] = mma32(va, pl[st], acc[ct]);
+            if (two_parts) acc[ct] = mma32(*reinterpret_cast<const u32x4*>(vt + kTileBytes + at), pw[st], acc[ct]);
+          }
+        }
     }
     __syncthreads();
   }
@@ -357,19 +388,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
       }
   }
   const int row = row0 + my_row;
-  if (row >= rows) return;
   const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
   if (a.splits > 1) {
-    float* rec = a.ws + (hq * a.splits + split) * kRec;
+    MergeWord* const word = a.words + (int64_t)tile * gridDim.x + blockIdx.x;
+    if (tid == 0) merge_announce(word, a.merge_tag);
+    if (row < rows) {
+      float* rec = a.ws + (hq * a.splits + split) * kRec;
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
+      for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4v*>(rec + 32 * ct + 8 * q + 4 * hh) =
-            float4v{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
-    if (hh == 0) { rec[kHeadDim] = m; rec[kHeadDim + 1] = l; }
+        for (int i = 0; i < 16; i += 2) store_record2(rec + 32 * ct + 8 * (i >> 2) + 4 * hh + (i & 3), acc[ct][i], acc[ct][i + 1]);
+      if (hh == 0) store_record2(rec + kHeadDim, m, l);
+    }
+    if (merge_arrive(word, a.merge_tag, a.splits, tid, &sm_last)) merge_rows<64 * kWaves>(a, b, h, row0, row_end - row0, tid);
     return;
   }
+  if (row >= rows) return;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;            // (a row that sees nothing: zeros)
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
@@ -381,31 +415,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
       for (int e = 0; e < 4; ++e) y[e] = acc[ct][4 * q + e] * inv;
       store_out4(a.out, a.out_dtype, o, y);
     }
-}
-
-// Joins the partial records of a row: one wavefront a row, two channels a lane.
-__global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t hq = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (hq >= (int64_t)a.g.batch * a.n_q * a.q_heads) return;
-  const int i = (int)(hq / a.q_heads % a.n_q), b = (int)(hq / a.q_heads / a.n_q);
-  if (a.q_lens && i >= a.q_lens[b]) return;                // rows behind the sequence's last stay as they are
-  const float* rec = a.ws + hq * a.splits * kRec;
-  float m = kNoMax;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, rec[s * kRec + kHeadDim]);
-  float l = 0.0f, x = 0.0f, y = 0.0f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float f = exp2f(rec[s * kRec + kHeadDim] - m);
-    l += f * rec[s * kRec + kHeadDim + 1];
-    x += f * rec[s * kRec + 2 * lane];
-    y += f * rec[s * kRec + 2 * lane + 1];
-  }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  x *= inv; y *= inv;
-  const int64_t o = hq * kHeadDim + 2 * lane;
-  if (a.out_dtype == KVQ_F32) *reinterpret_cast<float2*>((float*)a.out + o) = make_float2(x, y);
-  else if (a.out_dtype == KVQ_F16) { half2v u; u[0] = (_Float16)x; u[1] = (_Float16)y; *reinterpret_cast<uint32_t*>((uint16_t*)a.out + o) = as_u32(u); }
-  else *reinterpret_cast<uint32_t*>((uint16_t*)a.out + o) = f32_to_bf16_bits(x) | (uint32_t)f32_to_bf16_bits(y) << 16;
 }
 
 }  // namespace
@@ -437,7 +446,16 @@ size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t s
   return splits <= 1 ? 0 : (size_t)batch * n_q * q_heads * splits * kRec * sizeof(float);
 }
 
+size_t chunk_counter_bytes(const Geom& g, int heads_per_kv, int32_t n_q) {
+  const int64_t tiles = ((int64_t)n_q * heads_per_kv + 15) / 16;               // (16 rows: the smallest tile there is)
+  return (size_t)((tiles * g.batch * g.kv_heads * sizeof(MergeWord) + 15) / 16 * 16);
+}
+
 namespace {
+template <int NG> void launch_tiles(const ChunkArgs& a, dim3 grid, bool fine, hipStream_t stream) {
+  if (fine) hipLaunchKernelGGL((chunk_kernel<NG, true>), grid, dim3(64 * kWaves), 0, stream, a);
+  else hipLaunchKernelGGL((chunk_kernel<NG, false>), grid, dim3(64 * kWaves), 0, stream, a);
+}
 hipError_t launch_few(const ChunkArgs& a, int32_t sets, hipStream_t stream) {
   switch (32 * a.g.bits_k + a.g.bits_v) {
 #define KVQ_FEW_CASE(k, v) case 32 * k + v: return launch_few_k##k##v##v(a, sets, stream);
@@ -447,23 +465,22 @@ hipError_t launch_few(const ChunkArgs& a, int32_t sets, hipStream_t stream) {
 }
 }  // namespace
 
-hipError_t launch_chunk_attention(const ChunkArgs& a, int32_t few_sets, hipStream_t stream) {
-  if (few_sets) {
-    const hipError_t e = launch_few(a, few_sets, stream);
+hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, hipStream_t stream) {
+  ChunkArgs a = args;
+  if (a.splits > 1) a.merge_tag = next_merge_tag();
+  if (plan.few_sets) {
+    const hipError_t e = launch_few(a, plan.few_sets, stream);
     if (e != hipSuccess) return e;
   } else {
     const int tiles = (a.n_q * a.heads_per_kv + kTileRows - 1) / kTileRows;
     const dim3 grid(a.g.batch * a.g.kv_heads, tiles, a.splits);
+    const bool fine = a.out_dtype == KVQ_F32;
     switch (a.g.ng_k) {
-      case 1: hipLaunchKernelGGL((chunk_kernel<1>), grid, dim3(64 * kWaves), 0, stream, a); break;
-      case 2: hipLaunchKernelGGL((chunk_kernel<2>), grid, dim3(64 * kWaves), 0, stream, a); break;
-      case 4: hipLaunchKernelGGL((chunk_kernel<4>), grid, dim3(64 * kWaves), 0, stream, a); break;
+      case 1: launch_tiles<1>(a, grid, fine, stream); break;
+      case 2: launch_tiles<2>(a, grid, fine, stream); break;
+      case 4: launch_tiles<4>(a, grid, fine, stream); break;
       default: return hipErrorInvalidValue;
     }
-  }
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.g.batch * a.n_q * a.q_heads;
-    hipLaunchKernelGGL(chunk_merge_kernel, dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, a);
   }
   return hipGetLastError();
 }

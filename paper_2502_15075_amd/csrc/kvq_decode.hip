@@ -2213,7 +2213,7 @@ DecodePlan plan_decode(const Geom& g, int32_t seq_len, int heads, int64_t room, 
 constexpr int kMergeHereMost = 4, kMergeHereMostAlone = 2, kAloneHeads = 6;
 // The number such a launch carries (0: it does not merge): a greater one than all launches before it.  A replayed graph launch
 // carries its number again.
-static MergeWord next_merge_tag() {
+MergeWord next_merge_tag() {
   static std::atomic<MergeWord> launches{0};
   return merge_tag(launches.fetch_add(1, std::memory_order_relaxed));
 }

@@ -6,13 +6,13 @@ namespace kvq {
 
 // Column sets of 16 rows (query token, query head) a workgroup takes at most: three where their sums and a block's registers fit.
 constexpr int few_max_sets(int bits_k, int bits_v, int groups) { return bits_k + bits_v <= 8 && groups <= 2 ? 3 : 2; }
-constexpr int kFewWaves = 8;
 
+constexpr int kFewWaves = 8;
 template <int B> constexpr int key_loads() { return (32 * B + 63) / 64; }            // 16-byte loads of a lane for 32 key rows
 // Wavefronts per SIMD that the registers are cut for (512 of them a SIMD): the sums take 32 per column set, the next block 2 (b_K + b_V), the
 // rest about 80.
-template <int BK, int BV, int NC, int NG> constexpr int few_occupancy() {
-  constexpr bool odd = BK == 3 || BK == 6 || BV == 3 || BV == 6 || BK == 1 || BV == 1;          // (codes in two runs, lanes that share a word)
+constexpr int few_occupancy(int BK, int BV, int NC, int NG) {
+  const bool odd = BK == 3 || BK == 6 || BV == 3 || BV == 6 || BK == 1 || BV == 1;          // (codes in two runs, lanes that share a word)
   return NC > 1 || BK + BV > 16 || (NG == 4 && BK + BV > 12) ? 2 : NG == 4 || odd || BK + BV > 8 || (NG == 1 && BK + BV > 6) ? 3 : 4;
 }
 // LDS of a wavefront: a block's keys, values, scales and zeros
@@ -33,22 +33,22 @@ KVQ_FEW_PAIRS(KVQ_FEW_DECLARE)
 
 #if defined(__HIPCC__)
 // A lane's piece of a 32-token value block (16-byte pieces 1 KB apart; 1-bit fields: 8 bytes; 3 and 6 bits: low fields, then high ones)
-template <int B> __device__ __forceinline__ void load_value_piece(uint32_t* w, const uint8_t* block, int lane, uint32_t live) {
+template <int B> __device__ __forceinline__ void load_value_piece(uint32_t* w, const uint8_t* block, int lane) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   if constexpr (B == 3) {
-    load_value_piece<2>(w, block, lane, live);
-    load_value_piece<1>(w + 4, block + 1024, lane, live);
+    load_value_piece<2>(w, block, lane);
+    load_value_piece<1>(w + 4, block + 1024, lane);
   } else if constexpr (B == 6) {
-    load_value_piece<4>(w, block, lane, live);
-    load_value_piece<2>(w + 8, block + 2048, lane, live);
+    load_value_piece<4>(w, block, lane);
+    load_value_piece<2>(w + 8, block + 2048, lane);
   } else if constexpr (B == 1) {
-    const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(block + ((8u * lane) & live)));
+    const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(block + 8 * lane));
     w[0] = x[0]; w[1] = x[1];
   } else {
 #pragma unroll
     for (int i = 0; i < B / 2; ++i) {
-      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(block + ((1024u * i + 16u * lane) & live)));
+      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(block + 1024 * i + 16 * lane));
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
     }

@@ -14,7 +14,7 @@
 //
 // A code stays a number in the low bits of a binary16 lane, i.e. a subnormal: c 2^(k - 24) with its lowest bit at bit k, so that unpacking is a
 // shift and a mask; the power of two goes into the scores' factor and the final sums.  The matrix unit takes a subnormal by the exponent
-// 2^-14 and loses what lies 24 bits below a sum's largest product; k = 4 to 6 for narrow codes keeps that below binary32's own rounding.
+// 2^-14 and loses what lies 24 bits below a sum's largest product (code_base).
 //
 // A wavefront's next block is on its way while it computes one: its loads land in registers, and go from there through LDS of the
 // wavefront's own at the start of the next turn.  A lane needs 8 channels of every 32 of its key row (all groups alike), which would be loads
@@ -51,9 +51,10 @@ __device__ __forceinline__ float meta_z(uint32_t m) { return (float)as_half2(m)[
 template <int B> constexpr bool key_swizzled() { return (B & (B - 1)) == 0 && B > 1; }
 template <int B> __device__ __forceinline__ int key_swizzle(int row) { return key_swizzled<B>() ? (row * B / 16) & (B - 1) : 0; }
 
-// Where the lowest bit of a code lies in its binary16 lane.
-template <int B> constexpr int code_base() { return B == 1 || B == 2 ? 6 : B == 3 || B == 4 || B == 6 ? 4 : 0; }
-template <int B> constexpr float code_unit() { return B == 16 ? 1.0f : 1.0f / (float)(1 << (24 - code_base<B>())); }
+// Where the lowest bit k of a code lies in its binary16 lane.  2^(-14 - k) of a code's step is lost: for binary32 outputs (FINE) the codes go as high
+// as they fit, which leaves 2^-24 of a group's range whatever the width; otherwise where they need fewest shifts.
+template <int B, bool FINE> constexpr int code_base() { return FINE ? 10 - B : B == 1 || B == 2 ? 6 : B == 3 || B == 4 || B == 6 ? 4 : 0; }
+template <int B, bool FINE> constexpr float code_unit() { return B == 16 ? 1.0f : 1.0f / (float)(1 << (24 - code_base<B == 16 ? 8 : B, FINE>())); }
 // x >> n, n < 0: x << -n
 template <int N> __device__ __forceinline__ uint32_t shifted(uint32_t x) { return N >= 0 ? x >> (N >= 0 ? N : 0) : x << (N < 0 ? -N : 0); }
 // Fields of W bits at bits AT and 16 + AT of x, their lowest bits taken to BASE and 16 + BASE
@@ -62,8 +63,8 @@ template <int W, int AT, int BASE> __device__ __forceinline__ uint32_t field(uin
 }
 
 // Operand of channels 32 kk .. 32 kk + 31 of token row `row`: this lane's eight (slots 8 j .. 8 j + 7 of the chunk).
-template <int B> __device__ __forceinline__ u32x4 key_operand(const uint8_t* st, int row, int sw, int kk, int j, bool raw_bf) {
-  constexpr int K = code_base<B>();
+template <int B, bool FINE> __device__ __forceinline__ u32x4 key_operand(const uint8_t* st, int row, int sw, int kk, int j, bool raw_bf) {
+  constexpr int K = code_base<B == 16 ? 8 : B, FINE>();
   const uint8_t* base = st + row * (16 * B);
   if constexpr (B == 16) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(base + (((4 * kk + j) ^ sw) << 4));
@@ -96,8 +97,8 @@ template <int B> __device__ __forceinline__ u32x4 key_operand(const uint8_t* st,
 }
 
 // ---- value blocks: a lane's piece, 2 b dwords; field 4 dt + v is pair v (tokens 2 v, 2 v + 1 of the lane's eight) of channel tile dt
-template <int B> __device__ __forceinline__ u32x4 value_operand(const uint32_t* w, int dt) {
-  constexpr int K = code_base<B>();
+template <int B, bool FINE> __device__ __forceinline__ u32x4 value_operand(const uint32_t* w, int dt) {
+  constexpr int K = code_base<B == 16 ? 8 : B, FINE>();
   if constexpr (B == 16) return u32x4{w[4 * dt], w[4 * dt + 1], w[4 * dt + 2], w[4 * dt + 3]};
   else if constexpr (B == 8) return u32x4{field<8, 0, K>(w[2 * dt]), field<8, 8, K>(w[2 * dt]), field<8, 0, K>(w[2 * dt + 1]), field<8, 8, K>(w[2 * dt + 1])};
   else if constexpr (B == 4) return u32x4{field<4, 0, K>(w[dt]), field<4, 4, K>(w[dt]), field<4, 8, K>(w[dt]), field<4, 12, K>(w[dt])};
@@ -134,14 +135,15 @@ template <int BK, int BV> struct Step {
 
 // NG: the larger number of groups per row of the two tensors; a tensor with fewer is taken as one with NG whose scales repeat.
 template <int BK, int BV, int NC, int NG, bool FINE>
-__global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())) void few_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) void few_kernel(const ChunkArgs a) {
   constexpr int NW = kFewWaves, NK = key_loads<BK>(), kWaveBytes = few_wave_bytes<BK, BV>();
   constexpr bool RAWK = BK == 16, RAWV = BV == 16;
   constexpr bool kQueryInLds = NC > 1;
-  constexpr float kUnitK = code_unit<BK>(), kUnitV = code_unit<BV>();
+  constexpr float kUnitK = code_unit<BK, FINE>(), kUnitV = code_unit<BV, FINE>();
   __shared__ __attribute__((aligned(16))) uint8_t sm[few_lds_bytes<BK, BV, NC>()];
   __shared__ __attribute__((aligned(16))) uint8_t sm_query[16 * NC * 256];
   __shared__ __attribute__((aligned(16))) float sm_sums[16 * NC][4];
+  __shared__ int sm_last;
   __shared__ int sm_pos[16 * NC];                          // positions of the rows
   __shared__ float sm_kappa[16 * NC], sm_m[NW][16 * NC], sm_l[NW][16 * NC];
   const Geom& g = a.g;
@@ -179,15 +181,17 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
     k_off[i] = (uint32_t)(row * BK + ((u % BK) ^ key_swizzle<BK>(row))) * 16;
   }
   const int mu = min(lane, nmk + nmv - 1);
-  const int meta_token = 16 * (mu < nmk ? mu >= 4 * g.ng_k : mu - nmk >= 4 * g.ng_v) + 4 * (mu & 3);      // the first token of this lane's unit
-  const uint8_t* const meta_base = mu < nmk ? (const uint8_t*)a.cache.k_meta : (const uint8_t*)a.cache.v_meta;
-  const uint32_t meta_step = mu < nmk ? 128 * g.ng_k : 128 * g.ng_v, meta_off = 16 * (mu < nmk ? mu : mu - nmk);
+  // in LDS every tensor has NG groups: a tensor with fewer is stored once for each it stands for
+  const int ngk = RAWK ? 1 : g.ng_k, ngv = RAWV ? 1 : g.ng_v, rep = mu < nmk ? NG / ngk : NG / ngv, most_rep = NG / min(ngk, ngv);
+  const int unit = mu < nmk ? mu : mu - nmk, groups = mu < nmk ? ngk : ngv;
+  const int meta_at = (mu < nmk ? 0 : 128 * NG) + (unit / (4 * groups) * NG + (unit >> 2) % groups * rep) * 64 + (unit & 3) * 16;
+  const uintptr_t km = (uintptr_t)a.cache.k_meta, vm = (uintptr_t)a.cache.v_meta;
+  const uint32_t meta_off = 16 * unit;
   typedef const __attribute__((address_space(4))) int32_t* TablePtr;
   const TablePtr pages = (TablePtr)(uintptr_t)(g.page_shift ? a.cache.page_table + (int64_t)b * g.pages_per_seq : nullptr);
   const int page_blocks = g.page_shift - 5;
   auto page_of = [&](int blk) -> int { return g.page_shift ? pages[blk >> page_blocks] : 0; };
-  // (live = 0: a step that is not there; its loads collapse to one line)
-  auto load = [&](Step<BK, BV>& s, int blk, int page, uint32_t live) {
+  auto load = [&](Step<BK, BV>& s, int blk, int page) {
     const int64_t vb_ = g.page_shift ? (((int64_t)page * g.kv_heads + h) << page_blocks) + (blk & ((1 << page_blocks) - 1))
                                      : ((int64_t)b * g.kv_heads + h) * (g.t_cap >> 5) + blk;
     // (the choice above would leave the address in vector registers)
@@ -195,15 +199,15 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
     const uint8_t* kp = (const uint8_t*)a.cache.k_codes + vb * (512 * BK);
     const uint8_t* vp = (const uint8_t*)a.cache.v_codes + vb * (512 * BV);
 #pragma unroll
-    for (int i = 0; i < NK; ++i) s.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + (key_load_offset<BK>(k_off, i, lane) & live)));
-    load_value_piece<BV>(s.v, vp, lane, live);
+    for (int i = 0; i < NK; ++i) s.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + key_load_offset<BK>(k_off, i, lane)));
+    load_value_piece<BV>(s.v, vp, lane);
     if constexpr (RAWK && RAWV) s.meta = u32x4{0u, 0u, 0u, 0u};
-    else s.meta = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(meta_base + vb * meta_step + (meta_off & live)));
+    else s.meta = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((mu < nmk ? km + vb * (128 * g.ng_k) : vm + vb * (128 * g.ng_v)) + meta_off));
   };
 
   Step<BK, BV> step;
   const int x0 = begin + wave;                             // this wavefront's blocks: x0, x0 + NW, ...
-  if (x0 < end) load(step, block_at(x0), page_of(block_at(x0)), ~0u);
+  if (x0 < end) load(step, block_at(x0), page_of(block_at(x0)));
   int page = x0 + NW < end ? page_of(block_at(x0 + NW)) : 0;
   const int scale_exp = RAWV ? 0 : a.cache.v_scale_exp[(int64_t)b * g.kv_heads + h];
 
@@ -213,21 +217,16 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
   __syncthreads();
   auto query_operand = [&](int cs, int kk) { return *reinterpret_cast<const u32x4*>(sm_query + (16 * cs + c) * 256 + (((4 * kk + j) ^ c) << 4)); };
   u32x4 qb[kQueryInLds ? 1 : NC][4];
-  float qsum_[kQueryInLds ? 1 : NC][NG], kappa_[kQueryInLds ? 1 : NC];       // (more than one column set: read where they are used)
 #pragma unroll
   for (int cs = 0; cs < NC; ++cs) {
     if constexpr (!kQueryInLds) {
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) qb[cs][kk] = query_operand(cs, kk);
-#pragma unroll
-      for (int n = 0; n < NG; ++n) qsum_[cs][n] = sm_sums[16 * cs + c][n] * kUnitK;
-      kappa_[cs] = sm_kappa[16 * cs + c] * (1.0f / kUnitK);
     }
   }
-  auto query_sum = [&](int cs, int n) {                    // (scores carry the codes' unit)
-    if constexpr (kQueryInLds) return sm_sums[16 * cs + c][n] * kUnitK; else return qsum_[cs][n];
-  };
-  auto kappa = [&](int cs) { if constexpr (kQueryInLds) return sm_kappa[16 * cs + c] * (1.0f / kUnitK); else return kappa_[cs]; };
+  // (read where they are used: the loop has no registers for them.  Scores carry the codes' unit)
+  auto query_sum = [&](int cs, int n) { return sm_sums[16 * cs + c][n] * kUnitK; };
+  auto kappa = [&](int cs) { return sm_kappa[16 * cs + c] * (1.0f / kUnitK); };
   uint8_t* const st = sm + wave * kWaveBytes;
   uint8_t* const st_v = st + 512 * BK;
   uint8_t* const st_meta = st_v + 512 * BV;
@@ -235,11 +234,8 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
   // value scales of 64 and more take their bits of room from the weights
   const float weight_bits = kFewWeightBits - (float)max(scale_exp - 20, 0);
   const int sw = key_swizzle<BK>(c);
-  // where the scales and zeros of part n (of NG) of a row lie: group n >> shift of the tensor's
-  const int ngk = RAWK ? 1 : g.ng_k, ngv = RAWV ? 1 : g.ng_v;
-  const int shift_k = NG == ngk ? 0 : NG == 2 * ngk ? 1 : 2, shift_v = NG == ngv ? 0 : NG == 2 * ngv ? 1 : 2;
-  auto meta_k = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + ((x4 * ngk + (n >> shift_k)) * 16 + 4 * j) * 4); };
-  auto meta_v = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + 16 * nmk + ((x4 * ngv + (n >> shift_v)) * 16 + 4 * j) * 4); };
+  auto meta_k = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + 16 * j + (x4 * NG + n) * 64); };
+  auto meta_v = [&](int x4, int n) { return *reinterpret_cast<const u32x4*>(st_meta + 16 * j + 128 * NG + (x4 * NG + n) * 64); };
 
   float4v acc[NC][8];
   float m[NC], l[NC], zacc[NC][NG];
@@ -262,14 +258,15 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
     store_value_piece<BV>(step.v, st_v, lane);
     if constexpr (!RAWK || !RAWV) {
       if (tail) {                                          // (the sequence's last block: what lies behind its end is no number)
+        const int token = t0 + 16 * (meta_at % (128 * NG) / (64 * NG)) + ((meta_at >> 2) & 12);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) step.meta[r] = t0 + meta_token + r < limit ? step.meta[r] : 0u;
+        for (int r = 0; r < 4; ++r) step.meta[r] = token + r < limit ? step.meta[r] : 0u;
       }
-      *reinterpret_cast<u32x4*>(st_meta + 16 * lane) = step.meta;
+      *reinterpret_cast<u32x4*>(st_meta + meta_at) = step.meta;
+      for (int r = 1; r < most_rep; ++r) *reinterpret_cast<u32x4*>(st_meta + meta_at + 64 * min(r, rep - 1)) = step.meta;
     }
-    {
-      const bool more = x + NW < end;                      // uniform
-      load(step, block_at(more ? x + NW : x), more ? page : 0, more ? ~0u : 0u);
+    if (x + NW < end) {
+      load(step, block_at(x + NW), page);
       page = x + 2 * NW < end ? page_of(block_at(x + 2 * NW)) : 0;
     }
     __builtin_amdgcn_wave_barrier();
@@ -281,7 +278,7 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
       constexpr int NGK = RAWK ? 1 : NG;
       u32x4 ka[4];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) ka[kk] = key_operand<BK>(st, 16 * x4 + c, sw, kk, j, raw_bf);
+      for (int kk = 0; kk < 4; ++kk) ka[kk] = key_operand<BK, FINE>(st, 16 * x4 + c, sw, kk, j, raw_bf);
 #pragma unroll
       for (int cs = 0; cs < NC; ++cs)
 #pragma unroll
@@ -309,10 +306,12 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
     if (!whole) {
 #pragma unroll
       for (int cs = 0; cs < NC; ++cs) {
-        const int my_p = sm_pos[16 * cs + c], my_lo = a.window ? my_p - a.window : -1;
+        // (the lane's number formed anew: kept for this rare place it would cost the loop a register)
+        const int me = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), mj = me >> 4;
+        const int my_p = sm_pos[16 * cs + (me & 15)], my_lo = a.window ? my_p - a.window : -1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int t = t0 + 16 * (i >> 2) + 4 * j + (i & 3);
+          const int t = t0 + 16 * (i >> 2) + 4 * mj + (i & 3);
           const bool seen = (t <= my_p) & ((t > my_lo) | (t < a.sinks));
           sc[cs][i] = seen ? sc[cs][i] : -INFINITY;
         }
@@ -358,7 +357,7 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
             const uint32_t e0 = mv[i >> 1][2 * (i & 1)], e1 = mv[i >> 1][2 * (i & 1) + 1];
             zacc[cs][n] = fmaf(w0, meta_z(e0), zacc[cs][n]);
             zacc[cs][n] = fmaf(w1, meta_z(e1), zacc[cs][n]);
-            if constexpr (FINE) { w0 *= meta_s(e0); w1 *= meta_s(e1); }
+            if constexpr (FINE) { w0 = as_rounded(w0 * meta_s(e0)); w1 = as_rounded(w1 * meta_s(e1)); }
             else {                                         // (product and rounding in one instruction each)
               y[0] = (_Float16)fmaf(w0, meta_s(e0), 0.0f);
               y[1] = (_Float16)fmaf(w1, meta_s(e1), 0.0f);
@@ -375,7 +374,7 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
       }
 #pragma unroll
       for (int dt = n * (8 / NGV); dt < (n + 1) * (8 / NGV); ++dt) {
-        u32x4 va = value_operand<BV>(vw, dt);
+        u32x4 va = value_operand<BV, FINE>(vw, dt);
         if constexpr (RAWV) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -395,6 +394,10 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
     __builtin_amdgcn_wave_barrier();
   }
 
+  // (lane and thread formed anew: kept for here they would cost the loop a register)
+  const int me = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), my_tid = 64 * wave + me, mc = me & 15, mj = me >> 4;
+  MergeWord* const word = a.words + (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (a.splits > 1 && my_tid == 0) merge_announce(word, a.merge_tag);
   // ---- join the wavefronts: everybody's maxima and weight sums, then sums of channels rescaled to the common maximum
 #pragma unroll
   for (int cs = 0; cs < NC; ++cs) {
@@ -413,9 +416,9 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float o = __shfl_xor(y[r], 16);
-            y[r] = j & 1 ? o - y[r] : y[r] + o;
+            y[r] = mj & 1 ? o - y[r] : y[r] + o;
             o = __shfl_xor(y[r], 32);
-            y[r] = j & 2 ? o - y[r] : y[r] + o;
+            y[r] = mj & 2 ? o - y[r] : y[r] + o;
           }
         }
 #pragma unroll
@@ -428,11 +431,11 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float y = acc[cs][dt][r] * kRotScale;
-            acc[cs][dt][r] = (g.signs_v[dt >> 1] >> (16 * (dt & 1) + 4 * j + r)) & 1u ? -y : y;
+            acc[cs][dt][r] = (g.signs_v[dt >> 1] >> (16 * (dt & 1) + 4 * mj + r)) & 1u ? -y : y;
           }
       }
     }
-    if (j == 0) { sm_m[wave][16 * cs + c] = m[cs]; sm_l[wave][16 * cs + c] = l[cs]; }
+    if (mj == 0) { sm_m[wave][16 * cs + mc] = m[cs]; sm_l[wave][16 * cs + mc] = l[cs]; }
   }
   __syncthreads();
   constexpr int kParts = few_join_parts<NC>(), kWidth = kHeadDim / kParts, kStride = kWidth + 4;
@@ -442,19 +445,19 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
     if (part) __syncthreads();
 #pragma unroll
     for (int cs = 0; cs < NC; ++cs) {
-      float top = sm_m[0][16 * cs + c];
+      float top = sm_m[0][16 * cs + mc];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][16 * cs + c]);
+      for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][16 * cs + mc]);
       const float f = __builtin_amdgcn_exp2f(m[cs] - top);
 #pragma unroll
       for (int dt = part * (8 / kParts); dt < (part + 1) * (8 / kParts); ++dt)
-        *reinterpret_cast<float4v*>(sums + (wave * (16 * NC) + 16 * cs + c) * kStride + 16 * dt + 4 * j - part * kWidth) = acc[cs][dt] * f;
+        *reinterpret_cast<float4v*>(sums + (wave * (16 * NC) + 16 * cs + mc) * kStride + 16 * dt + 4 * mj - part * kWidth) = acc[cs][dt] * f;
     }
     __syncthreads();
     // 8 channels a thread, 16 (kParts = 2: 8) threads a row
     constexpr int kThreads = kWidth / 8;
-    for (int r = tid / kThreads; r < 16 * NC; r += 64 * NW / kThreads) {
-      const int d0 = 8 * (tid % kThreads), row = row0 + r;
+    for (int r = my_tid / kThreads; r < 16 * NC; r += 64 * NW / kThreads) {
+      const int d0 = 8 * (my_tid % kThreads), row = row0 + r;
       float top = sm_m[0][r], total = 0.0f;
 #pragma unroll
       for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][r]);
@@ -472,9 +475,9 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
         const int d = part * kWidth + d0;
         if (a.splits > 1) {
           float* rec = a.ws + (hq * a.splits + split) * kRec;
-          *reinterpret_cast<float4v*>(rec + d) = y0;
-          *reinterpret_cast<float4v*>(rec + d + 4) = y1;
-          if (d == 0) { rec[kHeadDim] = top; rec[kHeadDim + 1] = total; }
+          store_record2(rec + d, y0[0], y0[1]); store_record2(rec + d + 2, y0[2], y0[3]);
+          store_record2(rec + d + 4, y1[0], y1[1]); store_record2(rec + d + 6, y1[2], y1[3]);
+          if (d == 0) store_record2(rec + kHeadDim, top, total);
         } else {
           const float inv = total > 0.0f ? 1.0f / total : 0.0f;              // (a row that sees nothing: zeros)
           const float z0[4] = {y0[0] * inv, y0[1] * inv, y0[2] * inv, y0[3] * inv}, z1[4] = {y1[0] * inv, y1[1] * inv, y1[2] * inv, y1[3] * inv};
@@ -484,6 +487,8 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy<BK, BV, NC, NG>())
       }
     }
   }
+  if (a.splits > 1 && merge_arrive(word, a.merge_tag, a.splits, my_tid, &sm_last))
+    merge_rows<64 * NW>(a, b, h, row0, min(16 * NC, rows - row0), my_tid);
 }
 
 }  // namespace

@@ -88,6 +88,7 @@ struct AppendOne {
 };
 DecodePlan plan_decode(const Geom& g, int32_t seq_len, int heads, int64_t room, bool ragged);
 int32_t decode_records_bound(const Geom& g, int32_t seq_len, bool least = false);   // >= the records per head of every length up to seq_len
+MergeWord next_merge_tag();                                      // a launch's number for kvq_merge_count.h (of all launches of the process)
 int device_compute_units();                                      // of the current device (256 without one)
 
 // Everything the decode kernels need, passed by value.
@@ -137,13 +138,18 @@ struct ChunkArgs {
   int32_t seq_bound, window, sinks;
   float softmax_scale;
   void* out; int out_dtype;       // [B][n_q][q_heads][D]
-  float* ws; int32_t splits;      // parts a row's tokens are cut into; > 1: partial records in ws, joined by a second launch
+  // parts a row's tokens are cut into; > 1: partial records in ws, joined by the workgroup of a row tile that finishes last (the counters,
+  // one word per row tile, lie at `words`; kvq_merge_count.h has their rules)
+  float* ws; int32_t splits;
+  MergeWord* words; MergeWord merge_tag;
 };
 // How such a call is run: few_sets != 0: the kernel for a few rows, with that many column sets of 16 rows a workgroup; 0: tiles of rows.
 struct ChunkPlan { int32_t few_sets, splits; };
 ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks);
+// Bytes of the partial records (counters: of the counters behind them) of a call cut into `splits` parts; 0 for one part
 size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits);
-hipError_t launch_chunk_attention(const ChunkArgs& a, int32_t few_sets, hipStream_t stream);
+size_t chunk_counter_bytes(const Geom& g, int heads_per_kv, int32_t n_q);
+hipError_t launch_chunk_attention(const ChunkArgs& a, const ChunkPlan& plan, hipStream_t stream);
 
 // Append of several tokens per sequence with the rotation of their positions (kvq_rope_append).
 struct RopeArgs {

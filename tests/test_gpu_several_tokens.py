@@ -4,13 +4,14 @@ Appends are held byte for byte to the CPU oracle, which is given the keys rotate
 
 Attention is held to the formula in binary64 over the rows that kvq_dequantize returns, element by element, within
 
-    (3 * 2^-11 + 2 delta) * sum_t p_t |V^_t|  +  half a step of the output type,
+    (3 r + 2 delta) * sum_t p_t |V^_t|  +  r 2^-13 * sum_t |V^_t| / l  +  half a step of the output type,   l = sum_t p_t / p_max,
 
-because the kernels round every reconstructed value (or its weight, scale included) and every weight once to binary16, half a step 2^-11
-of it each, and the weights' sum follows the rounded weights (numerator and denominator: two more); delta is what the logits may be off
-by: 130 binary32 additions and the roundings of scale and exponent, 2^-24 each, of sums whose terms are bounded by sum_d |q_d| times the
-greatest |K^| (twice: codes and zeros are summed apart), taken 8 times for the cancellations inside a group (codes count from its minimum).
-Weights below 2^-24 of a row's largest (binary16's subnormals under the factor 2^10) lose bits: 2^-35 each of the largest.
+with r = 2^-11 for 16-bit outputs and 2^-21 for binary32 ones.  16-bit outputs: the kernels round every reconstructed value (or its weight,
+scale included) and every weight once to binary16, half a step 2^-11 of it each, and the weights' sum may follow the rounded weights or not
+(numerator and denominator: one more).  Binary32 outputs: weights and values travel as two binary16 parts, so that 2^-22 of each is lost, and the
+products are summed in binary32.  Weights far below a row's largest fall among binary16's subnormals: their step there is 2^-24 of a largest weight of
+at least 2^8, as are the steps of second parts.  delta is what the logits may be off by: 130 binary32 additions and the roundings of scale and
+exponent, 2^-24 each, of sums whose terms are bounded by sum_d |q_d| times the greatest |K^| (twice: codes and zeros are summed apart).
 """
 import math
 
@@ -125,8 +126,9 @@ def _reference(kvq, oracle, L, cache, q, q_lens, seq_lens, window, sinks, scale,
                 l = torch.where(l == 0, torch.ones_like(l), l)
                 want[b, :n, hq] = w @ v / l
                 mag = w @ v.abs() / l
-                delta = 8 * 2 * 132 * 2.0 ** -24 * scale * x.abs().sum(-1, keepdim=True) * k.abs().amax() / 16
-                tol[b, :n, hq] = (3 * 2.0 ** -11 + 2 * delta) * mag + 2.0 ** -35 * (seen.double() @ v.abs()) / l
+                delta = 2 * 132 * 2.0 ** -24 * scale * x.abs().sum(-1, keepdim=True) * k.abs().amax() / 2
+                r = 2.0 ** -21 if out_dtype == torch.float32 else 2.0 ** -11
+                tol[b, :n, hq] = (3 * r + 2 * delta) * mag + r * 2.0 ** -13 * (seen.double() @ v.abs()) / l
     tol += HALF_STEP[out_dtype] * want.abs().nan_to_num()
     return want, tol
 

@@ -23,7 +23,8 @@ def _good(kvq):
 def test_workspace_sizes(kvq):
     L = kvq.Layout(2, 8, 40000)
     one = kvq.chunk_workspace_bytes(L, 64, 1, 40000)
-    assert one > 0 and one % (2 * 64 * 132 * 4) == 0                # whole records of every row
+    counters = 2 * 8 * 8                                             # one word per (sequence, kv head) behind
+    assert one > counters and (one - counters) % (2 * 64 * 132 * 4) == 0       # whole records of every row
     assert kvq.window_workspace_bytes(L, 64, 40000, 0, 0) == one
     assert kvq.chunk_workspace_bytes(L, 64, 8192, 40000) == 0         # enough row tiles: nothing to cut
     assert kvq.chunk_workspace_bytes(L, 64, 0, 40000) == 0 and kvq.chunk_workspace_bytes(L, 64, 1, 0) == 0
