@@ -364,6 +364,7 @@ kvq_status chunk_common(const kvq_layout* layout, const kvq_cache* cache, const 
   const size_t counters = kvq::chunk_counter_bytes(a.g, a.heads_per_kv, n_q);
   const size_t room = workspace && workspace_bytes > counters ? (workspace_bytes - counters) / record : 0;
   if ((size_t)a.splits > room) a.splits = room < 2 ? 1 : (int32_t)room;
+  a.per = (plan.units + a.splits - 1) / a.splits;
   a.words = (kvq::MergeWord*)((char*)workspace + record * a.splits);
   return kvq::launch_chunk_attention(a, plan, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }

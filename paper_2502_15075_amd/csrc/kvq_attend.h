@@ -162,32 +162,32 @@ __device__ __forceinline__ bool merge_arrive(MergeWord* word, MergeWord tag, int
   __syncthreads();
   return *flag;
 }
-// Rows [row0, row0 + n) of a kv head from their records: 32 threads a row, four channels each, four records at a time under a running maximum.
+// Rows [row0, row0 + n) of a kv head from their `parts` records: 32 threads a row, four channels each, four records at a time under a running maximum.
 template <int THREADS>
-__device__ __forceinline__ void merge_rows(const ChunkArgs& a, int b, int h, int row0, int n, int tid) {
+__device__ __forceinline__ void merge_rows(const ChunkArgs& a, int b, int h, int row0, int n, int parts, int tid) {
   const int R = a.heads_per_kv;
   for (int idx = tid; idx < 32 * n; idx += THREADS) {
     const int row = row0 + (idx >> 5), d = 4 * (idx & 31);
     const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
     const float* rec = a.ws + hq * a.splits * kRec;
     float m = kNoMax, l = 0.0f, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+    for (int s0 = 0; s0 < parts; s0 += 4) {
       float2 ml[4], u[4], v[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float* r = rec + min(s0 + k, a.splits - 1) * kRec;
+        const float* r = rec + min(s0 + k, parts - 1) * kRec;
         ml[k] = load_record2(r + kHeadDim); u[k] = load_record2(r + d); v[k] = load_record2(r + d + 2);
       }
       float top = m;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) top = s0 + k < a.splits ? fmaxf(top, ml[k].x) : top;
+      for (int k = 0; k < 4; ++k) top = s0 + k < parts ? fmaxf(top, ml[k].x) : top;
       const float f0 = __builtin_amdgcn_exp2f(m - top);
       l *= f0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] *= f0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float f = s0 + k < a.splits ? __builtin_amdgcn_exp2f(ml[k].x - top) : 0.0f;
+        const float f = s0 + k < parts ? __builtin_amdgcn_exp2f(ml[k].x - top) : 0.0f;
         l = fmaf(f, ml[k].y, l);
         y[0] = fmaf(f, u[k].x, y[0]); y[1] = fmaf(f, u[k].y, y[1]); y[2] = fmaf(f, v[k].x, y[2]); y[3] = fmaf(f, v[k].y, y[3]);
       }

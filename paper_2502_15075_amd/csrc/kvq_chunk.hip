@@ -122,8 +122,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
   const int p0 = len - nq;                               // position of query token 0
   const int p_last = p0 + __builtin_amdgcn_readfirstlane((row_end - 1) / R);
   const Walk walk = make_walk(p0 + __builtin_amdgcn_readfirstlane(row0 / R), p_last, a.window, a.sinks);
-  const int per = __builtin_amdgcn_readfirstlane((walk.n + a.splits - 1) / a.splits);
-  const int t_begin = split * per, t_end = min(t_begin + per, walk.n);
+  const int parts = a.splits == 1 ? 1 : max(__builtin_amdgcn_readfirstlane((walk.n + a.per - 1) / a.per), 1);
+  if (split >= parts) return;                            // uniform
+  const int t_begin = split * a.per, t_end = min(t_begin + a.per, walk.n);
   const int limit = p_last + 1;                          // no row of the tile sees a token from here on
   const bool raw_bf = g.raw_dtype == KVQ_BF16;
   // Reconstructions may lie past binary16's largest number (code * scale + zero with a scale that was rounded up): results that overflow
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
   }
   const int row = row0 + my_row;
   const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
-  if (a.splits > 1) {
+  if (parts > 1) {
     MergeWord* const word = a.words + (int64_t)tile * gridDim.x + blockIdx.x;
     if (tid == 0) merge_announce(word, a.merge_tag);
     if (row < rows) {
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
         for (int i = 0; i < 16; i += 2) store_record2(rec + 32 * ct + 8 * (i >> 2) + 4 * hh + (i & 3), acc[ct][i], acc[ct][i + 1]);
       if (hh == 0) store_record2(rec + kHeadDim, m, l);
     }
-    if (merge_arrive(word, a.merge_tag, a.splits, tid, &sm_last)) merge_rows<64 * kWaves>(a, b, h, row0, row_end - row0, tid);
+    if (merge_arrive(word, a.merge_tag, parts, tid, &sm_last)) merge_rows<64 * kWaves>(a, b, h, row0, row_end - row0, parts, tid);
     return;
   }
   if (row >= rows) return;
@@ -423,19 +424,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
 // where there are fewer workgroups than compute units, as long as a part leaves every wavefront a few steps.
 constexpr int kFewRowsMax = 128;
 ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks) {
-  ChunkPlan plan{0, 1};
+  ChunkPlan plan{0, 1, 1};
   const int64_t rows = (int64_t)n_q * heads_per_kv, streams = (int64_t)g.batch * g.kv_heads;
-  int64_t span = seq_bound, splits;
-  if (window && span > (int64_t)window + sinks + n_q) span = (int64_t)window + sinks + n_q;
+  // the units (blocks of 32 tokens, tiles of 64) that a row tile of so many query tokens sees at most
+  auto units_of = [&](int64_t unit, int64_t tokens) {
+    int64_t all = (seq_bound + unit - 1) / unit;
+    if (window && tokens > n_q) tokens = n_q;
+    if (window) {
+      const int64_t some = ((int64_t)window + tokens - 1 + unit - 2) / unit + 1 + ((int64_t)sinks + unit - 1) / unit;
+      if (some < all) all = some;
+    }
+    return all < 1 ? 1 : all;
+  };
+  int64_t splits;
   if (rows <= kFewRowsMax) {
     const int ngk = g.bits_k == 16 ? 1 : g.ng_k, ngv = g.bits_v == 16 ? 1 : g.ng_v;
     const int most = few_max_sets(g.bits_k, g.bits_v, ngk > ngv ? ngk : ngv), sets = (int)((rows + 15) / 16);
-    plan.few_sets = (sets + (sets + most - 1) / most - 1) / ((sets + most - 1) / most);         // as few row tiles as can be, of the same size
-    const int64_t groups = streams * ((sets + plan.few_sets - 1) / plan.few_sets), blocks = (span + 31) / 32;
+    const int tiles = (sets + most - 1) / most;
+    plan.few_sets = (sets + tiles - 1) / tiles;            // as few row tiles as can be, of the same size
+    const int64_t groups = streams * tiles;
+    const int64_t blocks = units_of(32, 16 * plan.few_sets);
+    plan.units = (int32_t)blocks;
     splits = (plan.few_sets == 1 ? 2 : 1) * device_compute_units() / groups;
     if (splits > blocks / 16) splits = blocks / 16;
   } else {
-    const int64_t tiles = (rows + kTileRows - 1) / kTileRows * streams, steps = (span + kTileTokens - 1) / kTileTokens;
+    const int64_t tiles = (rows + kTileRows - 1) / kTileRows * streams, steps = units_of(kTileTokens, kTileRows);
+    plan.units = (int32_t)steps;
     splits = (2 * device_compute_units() + tiles - 1) / tiles;
     if (splits > steps / 4) splits = steps / 4;
   }

@@ -166,8 +166,9 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
   const int lo = a.window ? max(p_first - a.window + 1, 0) : 0;
   const int first = lo >> 5, sink_blocks = min((a.sinks + 31) >> 5, first);
   const int n_blocks = p_last >= 0 ? sink_blocks + (p_last >> 5) + 1 - first : 0;
-  const int per = a.splits == 1 ? n_blocks : __builtin_amdgcn_readfirstlane((n_blocks + a.splits - 1) / a.splits);
-  const int begin = split * per, end = min(begin + per, n_blocks);
+  const int parts = a.splits == 1 ? 1 : max(__builtin_amdgcn_readfirstlane((n_blocks + a.per - 1) / a.per), 1);
+  if (split >= parts) return;                              // uniform
+  const int begin = split * a.per, end = min(begin + a.per, n_blocks);
   auto block_at = [&](int x) { return x < sink_blocks ? x : x - sink_blocks + first; };
 
   // ---- loads of a step
@@ -182,11 +183,15 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
   }
   const int mu = min(lane, nmk + nmv - 1);
   // in LDS every tensor has NG groups: a tensor with fewer is stored once for each it stands for
-  const int ngk = RAWK ? 1 : g.ng_k, ngv = RAWV ? 1 : g.ng_v, rep = mu < nmk ? NG / ngk : NG / ngv, most_rep = NG / min(ngk, ngv);
-  const int unit = mu < nmk ? mu : mu - nmk, groups = mu < nmk ? ngk : ngv;
+  const int ngk = RAWK ? 1 : g.ng_k, ngv = RAWV ? 1 : g.ng_v, most_rep = NG / min(ngk, ngv);
+  const int unit = mu - (mu < nmk ? 0 : nmk), groups = ngk + (mu < nmk ? 0 : ngv - ngk);
+  const int rep = NG / groups;
   const int meta_at = (mu < nmk ? 0 : 128 * NG) + (unit / (4 * groups) * NG + (unit >> 2) % groups * rep) * 64 + (unit & 3) * 16;
-  const uintptr_t km = (uintptr_t)a.cache.k_meta, vm = (uintptr_t)a.cache.v_meta;
-  const uint32_t meta_off = 16 * unit;
+  // (picked by arithmetic: a choice between words of the argument block would become a load from it, waited for in every step.  A block number
+  // stays below 2^32: a block of value codes takes 512 bytes at least)
+  const uint64_t pick = mu < nmk ? 0 : ~0ull;
+  const uint64_t meta_base = (uint64_t)a.cache.k_meta + (((uint64_t)a.cache.v_meta - (uint64_t)a.cache.k_meta) & pick) + 16 * unit;
+  const uint32_t meta_step = 128 * g.ng_k + (128 * (g.ng_v - g.ng_k) & (uint32_t)pick);
   typedef const __attribute__((address_space(4))) int32_t* TablePtr;
   const TablePtr pages = (TablePtr)(uintptr_t)(g.page_shift ? a.cache.page_table + (int64_t)b * g.pages_per_seq : nullptr);
   const int page_blocks = g.page_shift - 5;
@@ -202,7 +207,7 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
     for (int i = 0; i < NK; ++i) s.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + key_load_offset<BK>(k_off, i, lane)));
     load_value_piece<BV>(s.v, vp, lane);
     if constexpr (RAWK && RAWV) s.meta = u32x4{0u, 0u, 0u, 0u};
-    else s.meta = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((mu < nmk ? km + vb * (128 * g.ng_k) : vm + vb * (128 * g.ng_v)) + meta_off));
+    else s.meta = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4*)(meta_base + (uint64_t)(uint32_t)vb * meta_step));
   };
 
   Step<BK, BV> step;
@@ -248,7 +253,17 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
     for (int n = 0; n < NG; ++n) zacc[cs][n] = 0.0f;
   }
 
+  // A SIMD serves its oldest wavefront first: of four with 24 steps each, bound by their instructions, the first was done after 45 us, the
+  // last, alone by then, after 84.  So the priority goes round, a step at each of four levels, wavefronts of a SIMD apart by their slot in it: 52 and
+  // 76 us (timing only: who computes what stays fixed).
+  uint32_t turn = __builtin_amdgcn_s_getreg((3 << 11) | 4);          // WAVE_ID, bits 3:0 of HW_ID
   for (int x = x0; x < end; x += NW) {
+    switch (turn++ & 3) {
+      case 0: __builtin_amdgcn_s_setprio(0); break;
+      case 1: __builtin_amdgcn_s_setprio(1); break;
+      case 2: __builtin_amdgcn_s_setprio(2); break;
+      default: __builtin_amdgcn_s_setprio(3); break;
+    }
     const int t0 = 32 * block_at(x);
     const bool tail = t0 + 32 > limit;
     // ---- the block to LDS, the next one under way
@@ -393,11 +408,12 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
     }
     __builtin_amdgcn_wave_barrier();
   }
+  __builtin_amdgcn_s_setprio(0);
 
   // (lane and thread formed anew: kept for here they would cost the loop a register)
   const int me = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), my_tid = 64 * wave + me, mc = me & 15, mj = me >> 4;
   MergeWord* const word = a.words + (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
-  if (a.splits > 1 && my_tid == 0) merge_announce(word, a.merge_tag);
+  if (parts > 1 && my_tid == 0) merge_announce(word, a.merge_tag);
   // ---- join the wavefronts: everybody's maxima and weight sums, then sums of channels rescaled to the common maximum
 #pragma unroll
   for (int cs = 0; cs < NC; ++cs) {
@@ -473,7 +489,7 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
       if (row < rows) {
         const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
         const int d = part * kWidth + d0;
-        if (a.splits > 1) {
+        if (parts > 1) {
           float* rec = a.ws + (hq * a.splits + split) * kRec;
           store_record2(rec + d, y0[0], y0[1]); store_record2(rec + d + 2, y0[2], y0[3]);
           store_record2(rec + d + 4, y1[0], y1[1]); store_record2(rec + d + 6, y1[2], y1[3]);
@@ -487,8 +503,8 @@ __global__ __launch_bounds__((64 * kFewWaves), (few_occupancy(BK, BV, NC, NG))) 
       }
     }
   }
-  if (a.splits > 1 && merge_arrive(word, a.merge_tag, a.splits, my_tid, &sm_last))
-    merge_rows<64 * NW>(a, b, h, row0, min(16 * NC, rows - row0), my_tid);
+  if (parts > 1 && merge_arrive(word, a.merge_tag, parts, my_tid, &sm_last))
+    merge_rows<64 * NW>(a, b, h, row0, min(16 * NC, rows - row0), parts, my_tid);
 }
 
 }  // namespace

@@ -138,13 +138,15 @@ struct ChunkArgs {
   int32_t seq_bound, window, sinks;
   float softmax_scale;
   void* out; int out_dtype;       // [B][n_q][q_heads][D]
-  // parts a row's tokens are cut into; > 1: partial records in ws, joined by the workgroup of a row tile that finishes last (the counters,
+  // parts a row's tokens are cut into at most, and the blocks (tiles, of 32 and 64 tokens) of a part: a row tile that sees fewer has fewer
+  // parts, so that all are about as long, whatever the sequences' lengths; > 1: partial records in ws, joined by the workgroup of a row tile that finishes last (the counters,
   // one word per row tile, lie at `words`; kvq_merge_count.h has their rules)
-  float* ws; int32_t splits;
+  float* ws; int32_t splits, per;
   MergeWord* words; MergeWord merge_tag;
 };
 // How such a call is run: few_sets != 0: the kernel for a few rows, with that many column sets of 16 rows a workgroup; 0: tiles of rows.
-struct ChunkPlan { int32_t few_sets, splits; };
+// units: the most blocks or tiles a row tile can see.
+struct ChunkPlan { int32_t few_sets, splits, units; };
 ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks);
 // Bytes of the partial records (counters: of the counters behind them) of a call cut into `splits` parts; 0 for one part
 size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits);
