@@ -24,27 +24,36 @@ namespace {
 constexpr float kWeightBits = 10.0f;     // weights carry 2^10: small ones stay clear of binary16's subnormals
 constexpr float kMaxSlack = 4.0f;        // the running maximum is raised once it lags by more: weights stay below 2^14
 constexpr int kTileTokens = 64;
-constexpr int kRowsPerWave = 32, kWaves = 4, kTileRows = kRowsPerWave * kWaves;
+constexpr int kRowsPerWave = 32;
 
 __device__ __forceinline__ float16v mma32(u32x4 a, u32x4 b, float16v c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
-// The codes of one 32-channel chunk (B dwords at p) as 16 binary16 pairs in slot order, four 16-byte pieces.
-template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* __restrict__ p, bool raw_bf, uint32_t one_k, u32x4 (&out)[4]) {
-  constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
-  constexpr int P = 16 / LO;                       // pairs per dword
-  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
-  uint32_t w[B];
+// One 32-channel chunk of a key row, B dwords, into registers ...
+template <int B> __device__ __forceinline__ void load_key_chunk(uint32_t* w, const uint32_t* __restrict__ p) {
   if constexpr (B % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < B / 4; ++i) *reinterpret_cast<u32x4*>(w + 4 * i) = reinterpret_cast<const u32x4*>(p)[i];
+    for (int i = 0; i < B / 4; ++i) {
+      const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+    }
+  } else if constexpr (B == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x; w[1] = x.y;
   } else {
 #pragma unroll
     for (int i = 0; i < B; ++i) w[i] = p[i];
   }
+}
+// ... and its codes as 16 binary16 pairs in slot order, four 16-byte pieces (PIECES 2: the first or the second half, B / 2 dwords).
+template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, uint32_t one_k, u32x4 (&out)[PIECES]) {
+  constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
+  constexpr int P = 16 / LO;                       // pairs per dword
+  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
 #pragma unroll
-  for (int s = 0; s < 16; ++s) {
+  for (int s = 0; s < 4 * PIECES; ++s) {
     const int dw = s / P, f = s % P;
     uint32_t x = w[dw] >> (LO * f);
     if constexpr (B == 16) {
@@ -63,13 +72,8 @@ template <int B> __device__ __forceinline__ void unpack_key_chunk(const uint32_t
   }
 }
 
-// The fields of LO bits of four 16-channel tiles (tiles 4 half .. 4 half + 3) of a lane's piece of a value block: pair v of tile
-// t is words' field 4 t + v.  out[4 t + v]: two codes, tokens 2 v and 2 v + 1 of the lane's eight.
-// MASKED: cut to the field (what is joined with high parts).
-template <int B, bool MASKED = false> __device__ __forceinline__ void value_fields(const uint32_t* __restrict__ block, int lane, int half, uint32_t (&out)[16]) {
-  constexpr int P = 16 / B;
-  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << B) - 1u) * 0x00010001u;
-  uint32_t w[B];
+// The B-bit fields of four 16-channel tiles (tiles 4 half .. 4 half + 3) of a lane's piece of a value block, B dwords ...
+template <int B> __device__ __forceinline__ void load_value_half(uint32_t* w, const uint32_t* __restrict__ block, int lane, int half) {
   if constexpr (B == 1) {
     w[0] = block[2 * lane + half];
   } else if constexpr (B == 2) {
@@ -77,11 +81,34 @@ template <int B, bool MASKED = false> __device__ __forceinline__ void value_fiel
     w[0] = x.x; w[1] = x.y;
   } else {
 #pragma unroll
-    for (int i = 0; i < B / 4; ++i)
-      *reinterpret_cast<u32x4*>(w + 4 * i) = *reinterpret_cast<const u32x4*>(block + 256 * (B / 4 * half + i) + 4 * lane);
-  }
+    for (int i = 0; i < B / 4; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(block + 256 * (B / 4 * half + i) + 4 * lane);
 #pragma unroll
-  for (int s = 0; s < 16; ++s) out[s] = MASKED ? (w[s / P] >> (B * (s % P))) & mask : w[s / P] >> (B * (s % P));
+      for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+    }
+  }
+}
+// ... as pairs: pair v of tile t is the words' field 4 t + v, tokens 2 v and 2 v + 1 of the lane's eight (with what lies above the field; MASKED: cut to
+// it, for what is joined with high parts).
+template <int B, bool MASKED = false, int N = 16> __device__ __forceinline__ void value_fields(const uint32_t* w, uint32_t (&out)[N]) {
+  constexpr int P = 16 / B;
+  constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << B) - 1u) * 0x00010001u;
+#pragma unroll
+  for (int s = 0; s < N; ++s) out[s] = MASKED ? (w[s / P] >> (B * (s % P))) & mask : w[s / P] >> (B * (s % P));
+}
+
+// N consecutive words, 1, 2 or 4, aligned to as many
+template <int N> __device__ __forceinline__ void load_words(uint32_t* w, const uint32_t* __restrict__ p) {
+  if constexpr (N == 4) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = x[e];
+  } else if constexpr (N == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x; w[1] = x.y;
+  } else {
+    w[0] = *p;
+  }
 }
 
 // What a workgroup walks: tokens [0, sink_tiles * 64) and [first * 64, ...), n tiles in all.
@@ -95,18 +122,21 @@ __device__ __forceinline__ Walk make_walk(int p_first, int p_last, int window, i
   return w;
 }
 
-template <int NG, bool FINE>
-__global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a) {
-  constexpr int kTileBytes = kTileTokens * kHeadDim * 2;
-  __shared__ __attribute__((aligned(16))) uint8_t sm_tile[(FINE ? 3 : 2) * kTileBytes];      // keys, values, the values' second parts
-  __shared__ __attribute__((aligned(16))) float sm_scale[4][kTileTokens];                      // key scales, by matrix row
-  __shared__ __attribute__((aligned(16))) uint32_t sm_zero[kTileTokens][4];                    // key zeros, each twice
+constexpr int tile_waves(int bk) { return bk ? 8 : 4; }
+
+// BK, BV: the widths, or 0 and 0: any, told at run time.  With widths known a thread's share of the next tile is loaded while this one is computed,
+// and 16-bit outputs have two tiles in LDS, one computed while the other is unpacked (binary32 ones, half as many again, one).
+template <int BK, int BV, int NG, bool FINE>
+__global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const ChunkArgs a) {
+  constexpr bool kAhead = BK != 0;
+  constexpr int kWaves = tile_waves(BK), kTileRows = kRowsPerWave * kWaves;
+  constexpr int kTileBytes = kTileTokens * kHeadDim * 2, kBuffers = kAhead ? 2 : 1, kBufferBytes = (FINE ? 3 : 2) * kTileBytes;
+  __shared__ __attribute__((aligned(16))) uint8_t sm_tile[kBuffers * kBufferBytes];            // keys, values, the values' second parts
+  __shared__ __attribute__((aligned(16))) float sm_scale_[kBuffers][4][kTileTokens];           // key scales, by matrix row
+  __shared__ __attribute__((aligned(16))) uint32_t sm_zero_[kBuffers][kTileTokens][4];         // key zeros, each twice
   __shared__ __attribute__((aligned(16))) uint32_t sm_qsum[kTileRows][4];                      // group sums of the query, two parts each
   __shared__ float sm_kappa[kTileRows];
   __shared__ int sm_last;
-  uint8_t* const sm_k = sm_tile;
-  uint8_t* const sm_v = sm_tile + kTileBytes;
-
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // (a division leaves its result in vector registers, and with it every address: these are the same in all lanes)
@@ -158,114 +188,93 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
   const bool two_parts = g.bits_v != 16;                   // (patterns of an unquantized plane have no second part)
   const uint32_t one_k = one_k_pattern(), v_mask = ((1u << min(g.bits_v, 15)) - 1u) * 0x00010001u;
 
-  for (int ti = t_begin; ti < t_end; ++ti) {
-    const int t0 = (ti < walk.sink_tiles ? ti : walk.first + ti - walk.sink_tiles) * kTileTokens;
-    // ---- unpack the tile
-    // (paged: a tile never straddles a page)
-    const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0);      // plane order's number of the tile's first token
-    {
-      const int tok = tid >> 2, chunk = tid & 3;
-      const int src = min(t0 + tok, limit - 1) - t0;                           // (nothing behind the last visible token is read)
-      const int x = tok & 31, row = (tok & 32) | (x & 7) | ((x & 8) << 1) | ((x & 16) >> 1);   // bits 3 and 4 swapped
-      u32x4 piece[4];
-      const uint32_t* kp = (const uint32_t*)a.cache.k_codes + (base + src) * (4 * g.bits_k) + chunk * g.bits_k;
-      switch (g.bits_k) {
-        case 1: unpack_key_chunk<1>(kp, raw_bf, one_k, piece); break;
-        case 2: unpack_key_chunk<2>(kp, raw_bf, one_k, piece); break;
-        case 3: unpack_key_chunk<3>(kp, raw_bf, one_k, piece); break;
-        case 4: unpack_key_chunk<4>(kp, raw_bf, one_k, piece); break;
-        case 6: unpack_key_chunk<6>(kp, raw_bf, one_k, piece); break;
-        case 8: unpack_key_chunk<8>(kp, raw_bf, one_k, piece); break;
-        default: unpack_key_chunk<16>(kp, raw_bf, one_k, piece); break;
-      }
+  // (a block of tiles: [0, sink_tiles) and [first, ...))
+  auto first_token = [&](int ti) { return (ti < walk.sink_tiles ? ti : walk.first + ti - walk.sink_tiles) * kTileTokens; };
+  // Thread t unpacks, of token `tok`, part `chunk` of its key row, and tiles 4 half ... of value block `vblk` as lane (j, dl) of a fragment; with
+  // eight wavefronts half as much: the part's half `sub`, tiles 2 half ... .
+  constexpr int kPieces = kAhead ? 2 : 4, kTiles = kAhead ? 2 : 4, kPairs = 4 * kTiles;
+  const int tok = tid / (16 / kPieces), sub = kAhead ? tid & 1 : 0, chunk = (tid >> (kAhead ? 1 : 0)) & 3;
+  const int vblk = tid / (128 * 4 / kTiles), half = (tid >> 6) & (8 / kTiles - 1), j = lane >> 4, dl = lane & 15;
+  const int x_ = tok & 31, k_row = (tok & 32) | (x_ & 7) | ((x_ & 8) << 1) | ((x_ & 16) >> 1);        // bits 3 and 4 swapped
+  const int per_group = g.g_v >> 4;                        // 16-channel tiles of a value group
+  auto key_source = [&](int t0, int64_t base) { return base + (min(t0 + tok, limit - 1) - t0); };      // (nothing behind the last visible token is read)
+  auto value_source = [&](int t0, int64_t base) { return (base >> 5) + (min((t0 >> 5) + vblk, (limit - 1) >> 5) - (t0 >> 5)); };
+  auto load_metas = [&](int64_t src, int64_t vsrc, bool raw_k, bool raw_v, uint32_t& km, u32x4 (&vm)[kTiles]) {
+    km = raw_k ? 0x00003C00u : ((const uint32_t*)a.cache.k_meta)[meta_index(src, min(chunk, NG - 1), NG)];                 // (unquantized: scale 1, zero 0)
+    if (raw_v) return;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<u32x4*>(sm_k + row * 256 + (((4 * chunk + i) ^ (row & 15)) << 4)) = piece[i];
-      uint32_t meta = 0;
-      if (g.bits_k == 16) meta = 0x00003C00u;                                  // scale 1, zero 0
-      else if (chunk < NG) meta = ((const uint32_t*)a.cache.k_meta)[meta_index(base + src, chunk, NG)];
-      if (t0 + tok >= limit || chunk >= NG) meta = 0;
-      sm_scale[chunk][row] = widen16((uint16_t)meta, false);
-      sm_zero[row][chunk] = (meta >> 16) * 0x00010001u;
+    for (int n = 0; n < kTiles / 2; ++n) {
+      if (n == 1 && per_group != 2) break;                 // uniform: half a row is one group, or two
+      const uint32_t* mp = (const uint32_t*)a.cache.v_meta + meta_index(32 * vsrc, (kTiles * half + 2 * n) / per_group, g.ng_v) + 4 * j;
+#pragma unroll
+      for (int x4 = 0; x4 < 2; ++x4) vm[2 * n + x4] = *reinterpret_cast<const u32x4*>(mp + 16 * g.ng_v * x4);
     }
-    {
-      const int blk = tid >> 7, half = (tid >> 6) & 1;
-      const int sblk = min((t0 >> 5) + blk, (limit - 1) >> 5) - (t0 >> 5);
-      const uint32_t* vp = (const uint32_t*)a.cache.v_codes + ((base >> 5) + sblk) * (128 * g.bits_v);
-      uint32_t f[16];
-      switch (g.bits_v) {
-        case 1: value_fields<1>(vp, lane, half, f); break;
-        case 2: value_fields<2>(vp, lane, half, f); break;
-        case 4: value_fields<4>(vp, lane, half, f); break;
-        case 8: value_fields<8>(vp, lane, half, f); break;
-        case 16: value_fields<16>(vp, lane, half, f); break;
-        default: {                                         // 3 and 6 bits: a block of low parts, a block of high parts
-          uint32_t hi[16];
-          if (g.bits_v == 3) {
-            value_fields<2, true>(vp, lane, half, f); value_fields<1, true>(vp + 256, lane, half, hi);
-          } else {
-            value_fields<4, true>(vp, lane, half, f); value_fields<2, true>(vp + 512, lane, half, hi);
-          }
-          const int lo = g.bits_v == 3 ? 2 : 4;
+  };
+  auto store = [&](const u32x4 (&piece)[kPieces], uint32_t km, uint32_t (&f)[kPairs], u32x4 (&vm)[kTiles], bool raw_v, int t0, int at) {
+    uint8_t* const sm_k = sm_tile + at * kBufferBytes;
+    uint8_t* const sm_v = sm_k + kTileBytes + vblk * 8192 + (j * 128 + 16 * kTiles * half + dl) * 16;
 #pragma unroll
-          for (int s = 0; s < 16; ++s) f[s] |= hi[s] << lo;
-        }
+    for (int i = 0; i < kPieces; ++i)
+      *reinterpret_cast<u32x4*>(sm_k + k_row * 256 + (((4 * chunk + kPieces * sub + i) ^ (k_row & 15)) << 4)) = piece[i];
+    if (t0 + tok >= limit || chunk >= NG) km = 0;
+    sm_scale_[at][chunk][k_row] = widen16((uint16_t)km, false);
+    sm_zero_[at][k_row][chunk] = (km >> 16) * 0x00010001u;
+
+    const int valid = limit - (t0 + 32 * vblk + 4 * j);    // of tokens 16 x4 + 4 j + r those with 16 x4 + r < valid are visible to some row
+    if (raw_v) {
+#pragma unroll
+      for (int s = 0; s < kPairs; ++s) {
+        const int token = 16 * ((s & 2) >> 1) + 2 * (s & 1);       // pair v = s % 4: tokens 2 v, 2 v + 1 of the eight (x4, r)
+        uint32_t x = raw_to_half2(f[s], raw_bf);
+        if (token >= valid) x &= 0xFFFF0000u;
+        if (token + 1 >= valid) x &= 0x0000FFFFu;
+        f[s] = x;
       }
-      const int j = lane >> 4, dl = lane & 15;
-      const int valid = limit - (t0 + 32 * blk + 4 * j);   // of tokens 16 x4 + 4 j + r those with 16 x4 + r < valid are visible to some row
-      if (g.bits_v == 16) {
+    } else {
+      if (t0 + kTileTokens > limit) {                      // uniform: the last tile (what lies behind the end is no number)
 #pragma unroll
-        for (int s = 0; s < 16; ++s) {
-          const int at = 16 * ((s & 2) >> 1) + 2 * (s & 1);    // pair v = s % 4: tokens 2 v, 2 v + 1 of the eight (x4, r)
-          uint32_t x = raw_to_half2(f[s], raw_bf);
-          if (at >= valid) x &= 0xFFFF0000u;
-          if (at + 1 >= valid) x &= 0x0000FFFFu;
-          f[s] = x;
-        }
-      } else {
-        const int per_group = g.g_v >> 4;                  // 16-channel tiles of a group
-        u32x4 m4[2];
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int dt = 4 * half + t;
-          u32x4 second;
-          if (t == 0 || (t == 2 && per_group == 2)) {
-            const int gr = dt / per_group;
-            const uint32_t* mp = (const uint32_t*)a.cache.v_meta + meta_index(base + 32 * sblk, gr, g.ng_v) + 4 * j;
+          for (int r = 0; r < 4; ++r)
+            if (16 * (i & 1) + r >= valid) vm[i][r] = 0u;
+      }
+      half2v sc[4], ze[4];                                 // scales and zeros of the four pairs
 #pragma unroll
-            for (int x4 = 0; x4 < 2; ++x4) {
-              m4[x4] = *reinterpret_cast<const u32x4*>(mp + 16 * g.ng_v * x4);
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (16 * x4 + r >= valid) m4[x4][r] = 0u;
-            }
-          }
+      for (int t = 0; t < kTiles; ++t) {
+        u32x4 second;
+        if (t == 0 || (t == 2 && per_group == 2)) {
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const uint32_t e0 = m4[v >> 1][2 * (v & 1)], e1 = m4[v >> 1][2 * (v & 1) + 1];
-            const half2v s = as_half2((e0 & 0xFFFFu) | (e1 << 16)), z = as_half2((e0 >> 16) | (e1 & 0xFFFF0000u));
-            const half2v code = whole_to_half2(f[4 * t + v], v_mask, one_k);
-            if constexpr (FINE) {
-              const float x = as_rounded(fmaf((float)code[0], (float)s[0], (float)z[0])), y = as_rounded(fmaf((float)code[1], (float)s[1], (float)z[1]));
-              half2v hi, lo;
-              hi[0] = (_Float16)x; hi[1] = (_Float16)y;
-              lo[0] = (_Float16)(x - (float)hi[0]); lo[1] = (_Float16)(y - (float)hi[1]);
-              f[4 * t + v] = as_u32(hi);
-              second[v] = as_u32(lo);
-            } else {
-              f[4 * t + v] = as_u32(__builtin_elementwise_fma(code, s, z));
-            }
+            const uint32_t e0 = vm[t + (v >> 1)][2 * (v & 1)], e1 = vm[t + (v >> 1)][2 * (v & 1) + 1];
+            sc[v] = as_half2(__builtin_amdgcn_perm(e1, e0, 0x05040100u));      // low halves
+            ze[v] = as_half2(__builtin_amdgcn_perm(e1, e0, 0x07060302u));      // high halves
           }
-          if constexpr (FINE) *reinterpret_cast<u32x4*>(sm_v + kTileBytes + blk * 8192 + (j * 128 + 16 * dt + dl) * 16) = second;
         }
-      }
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        *reinterpret_cast<u32x4*>(sm_v + blk * 8192 + (j * 128 + 16 * (4 * half + t) + dl) * 16) =
-            u32x4{f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]};
+        for (int v = 0; v < 4; ++v) {
+          const half2v code = whole_to_half2(f[4 * t + v], v_mask, one_k);
+          if constexpr (FINE) {
+            const float x = as_rounded(fmaf((float)code[0], (float)sc[v][0], (float)ze[v][0]));
+            const float y = as_rounded(fmaf((float)code[1], (float)sc[v][1], (float)ze[v][1]));
+            half2v hi, lo;
+            hi[0] = (_Float16)x; hi[1] = (_Float16)y;
+            lo[0] = (_Float16)(x - (float)hi[0]); lo[1] = (_Float16)(y - (float)hi[1]);
+            f[4 * t + v] = as_u32(hi);
+            second[v] = as_u32(lo);
+          } else {
+            f[4 * t + v] = as_u32(__builtin_elementwise_fma(code, sc[v], ze[v]));
+          }
+        }
+        if constexpr (FINE) *reinterpret_cast<u32x4*>(sm_v + kTileBytes + 256 * t) = second;
+      }
     }
-    __syncthreads();
-
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) *reinterpret_cast<u32x4*>(sm_v + 256 * t) = u32x4{f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]};
+  };
+  auto compute = [&](int ti, int at) {
+    const int t0 = first_token(ti);
+    const uint8_t* const sm_k = sm_tile + at * kBufferBytes;
+    const uint8_t* const sm_v = sm_k + kTileBytes;
     // ---- two blocks of 32 tokens
 #pragma unroll
     for (int blk = 0; blk < 2; ++blk) {
@@ -277,7 +286,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
         float16v zero;
 #pragma unroll
         for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
-        s = mma32(*reinterpret_cast<const u32x4*>(sm_zero[32 * blk + col]), qs, zero);
+        s = mma32(*reinterpret_cast<const u32x4*>(sm_zero_[at][32 * blk + col]), qs, zero);
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
           float16v part = zero;
@@ -286,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
             part = mma32(*reinterpret_cast<const u32x4*>(kt + col * 256 + (((2 * kk + hh) ^ (col & 15)) << 4)), qb[kk], part);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const float4v sc = *reinterpret_cast<const float4v*>(&sm_scale[n][32 * blk + 8 * q + 4 * hh]);
+            const float4v sc = *reinterpret_cast<const float4v*>(&sm_scale_[at][n][32 * blk + 8 * q + 4 * hh]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(sc[e], part[4 * q + e], s[4 * q + e]);
           }
@@ -347,7 +356,88 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
           }
         }
     }
-    __syncthreads();
+  };
+
+  if constexpr (kAhead) {
+    uint32_t raw_k[BK / 2], raw_v[BV / 2], raw_km;         // what a thread loads of a tile (paged: a tile never straddles a page)
+    u32x4 raw_vm[kTiles];
+    auto load = [&](int ti) {
+      const int t0 = first_token(ti);
+      const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0), src = key_source(t0, base), vsrc = value_source(t0, base);
+      load_words<BK / 2>(raw_k, (const uint32_t*)a.cache.k_codes + src * (4 * BK) + chunk * BK + sub * (BK / 2));
+      constexpr int kWords = BV / 2;                         // of the lane's 2 BV, which lie in fours: 256 words from one four to the next
+      const int w = kWords * half;
+      load_words<kWords>(raw_v, (const uint32_t*)a.cache.v_codes + vsrc * (128 * BV) + 256 * (w >> 2) + 4 * lane + (w & 3));
+      load_metas(src, vsrc, false, false, raw_km, raw_vm);
+    };
+    // The loaded tile, to buffer `at`
+    auto unpack = [&](int ti, int at) {
+      u32x4 piece[kPieces];
+      uint32_t f[kPairs];
+      unpack_key_chunk<BK, kPieces>(raw_k, raw_bf, one_k, piece);
+      value_fields<BV, false, kPairs>(raw_v, f);
+      store(piece, raw_km, f, raw_vm, false, first_token(ti), at);
+    };
+    if (t_begin < t_end) {
+      load(t_begin);
+      unpack(t_begin, 0);
+      if (t_begin + 1 < t_end) load(t_begin + 1);
+      __syncthreads();
+    }
+    for (int ti = t_begin; ti < t_end; ++ti) {
+      const int at = (ti - t_begin) & 1;
+      compute(ti, at);
+      if (ti + 1 < t_end) unpack(ti + 1, 1 - at);
+      if (ti + 2 < t_end) load(ti + 2);
+      __syncthreads();
+    }
+  } else {
+    // A tile of widths told at run time
+    auto load_and_unpack = [&](int ti) {
+      const int t0 = first_token(ti), bits_k = g.bits_k, bits_v = g.bits_v;
+      const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0), src = key_source(t0, base), vsrc = value_source(t0, base);
+      const uint32_t* kp = (const uint32_t*)a.cache.k_codes + src * (4 * bits_k) + chunk * bits_k;
+      const uint32_t* vp = (const uint32_t*)a.cache.v_codes + vsrc * (128 * bits_v);
+      u32x4 piece[4], vm[4];
+      uint32_t w[16], f[16], km;
+      switch (bits_k) {
+        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1>(w, raw_bf, one_k, piece); break;
+        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2>(w, raw_bf, one_k, piece); break;
+        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3>(w, raw_bf, one_k, piece); break;
+        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4>(w, raw_bf, one_k, piece); break;
+        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6>(w, raw_bf, one_k, piece); break;
+        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8>(w, raw_bf, one_k, piece); break;
+        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16>(w, raw_bf, one_k, piece); break;
+      }
+      switch (bits_v) {
+        case 1: load_value_half<1>(w, vp, lane, half); value_fields<1>(w, f); break;
+        case 2: load_value_half<2>(w, vp, lane, half); value_fields<2>(w, f); break;
+        case 4: load_value_half<4>(w, vp, lane, half); value_fields<4>(w, f); break;
+        case 8: load_value_half<8>(w, vp, lane, half); value_fields<8>(w, f); break;
+        case 16: load_value_half<16>(w, vp, lane, half); value_fields<16>(w, f); break;
+        default: {                                           // 3 and 6 bits: a block of low parts, a block of high parts
+          uint32_t hi[16];
+          if (bits_v == 3) {
+            load_value_half<2>(w, vp, lane, half); value_fields<2, true>(w, f);
+            load_value_half<1>(w, vp + 256, lane, half); value_fields<1, true>(w, hi);
+          } else {
+            load_value_half<4>(w, vp, lane, half); value_fields<4, true>(w, f);
+            load_value_half<2>(w, vp + 512, lane, half); value_fields<2, true>(w, hi);
+          }
+          const int lo = bits_v == 3 ? 2 : 4;
+#pragma unroll
+          for (int s = 0; s < 16; ++s) f[s] |= hi[s] << lo;
+        }
+      }
+      load_metas(src, vsrc, bits_k == 16, bits_v == 16, km, vm);
+      store(piece, km, f, vm, bits_v == 16, t0, 0);
+    };
+    for (int ti = t_begin; ti < t_end; ++ti) {
+      load_and_unpack(ti);
+      __syncthreads();
+      compute(ti, 0);
+      __syncthreads();
+    }
   }
 
   // ---- results.  acc[ct][i]: channel 32 ct + 8 (i / 4) + 4 hh + i % 4 of row `col`
@@ -423,6 +513,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(const ChunkArgs a
 // Up to kFewRowsMax rows of a kv head go to the kernel that keeps the cache packed, more to the tiles above.  The tokens are cut into parts
 // where there are fewer workgroups than compute units, as long as a part leaves every wavefront a few steps.
 constexpr int kFewRowsMax = 128;
+// (the widths of every day have tiles of 256 rows, all others share the kernel without widths)
+bool tile_widths(int bk, int bv) { return (bk == 2 || bk == 4 || bk == 8) && (bv == 2 || bv == 4 || bv == 8); }
+int tile_rows(const Geom& g) { return kRowsPerWave * tile_waves(tile_widths(g.bits_k, g.bits_v) ? g.bits_k : 0); }
 ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks) {
   ChunkPlan plan{0, 1, 1};
   const int64_t rows = (int64_t)n_q * heads_per_kv, streams = (int64_t)g.batch * g.kv_heads;
@@ -448,9 +541,10 @@ ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_b
     splits = (plan.few_sets == 1 ? 2 : 1) * device_compute_units() / groups;
     if (splits > blocks / 16) splits = blocks / 16;
   } else {
-    const int64_t tiles = (rows + kTileRows - 1) / kTileRows * streams, steps = units_of(kTileTokens, kTileRows);
+    const int at_once = tile_rows(g);
+    const int64_t tiles = (rows + at_once - 1) / at_once * streams, steps = units_of(kTileTokens, at_once);
     plan.units = (int32_t)steps;
-    splits = (2 * device_compute_units() + tiles - 1) / tiles;
+    splits = (256 / at_once * device_compute_units() + tiles - 1) / tiles;
     if (splits > steps / 4) splits = steps / 4;
   }
   plan.splits = (int32_t)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
@@ -466,9 +560,17 @@ size_t chunk_counter_bytes(const Geom& g, int heads_per_kv, int32_t n_q) {
 }
 
 namespace {
-template <int NG> void launch_tiles(const ChunkArgs& a, dim3 grid, bool fine, hipStream_t stream) {
-  if (fine) hipLaunchKernelGGL((chunk_kernel<NG, true>), grid, dim3(64 * kWaves), 0, stream, a);
-  else hipLaunchKernelGGL((chunk_kernel<NG, false>), grid, dim3(64 * kWaves), 0, stream, a);
+template <int BK, int BV, int NG> void launch_tiles(const ChunkArgs& a, dim3 grid, hipStream_t stream) {
+  if (a.out_dtype == KVQ_F32) hipLaunchKernelGGL((chunk_kernel<BK, BV, NG, true>), grid, dim3(64 * tile_waves(BK)), 0, stream, a);
+  else hipLaunchKernelGGL((chunk_kernel<BK, BV, NG, false>), grid, dim3(64 * tile_waves(BK)), 0, stream, a);
+}
+template <int BK, int BV> hipError_t launch_tiles_of(const ChunkArgs& a, dim3 grid, hipStream_t stream) {
+  switch (a.g.ng_k) {
+    case 1: launch_tiles<BK, BV, 1>(a, grid, stream); return hipSuccess;
+    case 2: launch_tiles<BK, BV, 2>(a, grid, stream); return hipSuccess;
+    case 4: launch_tiles<BK, BV, 4>(a, grid, stream); return hipSuccess;
+  }
+  return hipErrorInvalidValue;
 }
 hipError_t launch_few(const ChunkArgs& a, int32_t sets, hipStream_t stream) {
   switch (32 * a.g.bits_k + a.g.bits_v) {
@@ -486,15 +588,22 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
     const hipError_t e = launch_few(a, plan.few_sets, stream);
     if (e != hipSuccess) return e;
   } else {
-    const int tiles = (a.n_q * a.heads_per_kv + kTileRows - 1) / kTileRows;
+    const int at_once = tile_rows(a.g), tiles = (a.n_q * a.heads_per_kv + at_once - 1) / at_once;
     const dim3 grid(a.g.batch * a.g.kv_heads, tiles, a.splits);
-    const bool fine = a.out_dtype == KVQ_F32;
-    switch (a.g.ng_k) {
-      case 1: launch_tiles<1>(a, grid, fine, stream); break;
-      case 2: launch_tiles<2>(a, grid, fine, stream); break;
-      case 4: launch_tiles<4>(a, grid, fine, stream); break;
-      default: return hipErrorInvalidValue;
+    hipError_t e;
+    switch (32 * a.g.bits_k + a.g.bits_v) {                // 
+      case 32 * 2 + 2: e = launch_tiles_of<2, 2>(a, grid, stream); break;
+      case 32 * 2 + 4: e = launch_tiles_of<2, 4>(a, grid, stream); break;
+      case 32 * 4 + 2: e = launch_tiles_of<4, 2>(a, grid, stream); break;
+      case 32 * 4 + 4: e = launch_tiles_of<4, 4>(a, grid, stream); break;
+      case 32 * 2 + 8: e = launch_tiles_of<2, 8>(a, grid, stream); break;
+      case 32 * 4 + 8: e = launch_tiles_of<4, 8>(a, grid, stream); break;
+      case 32 * 8 + 2: e = launch_tiles_of<8, 2>(a, grid, stream); break;
+      case 32 * 8 + 4: e = launch_tiles_of<8, 4>(a, grid, stream); break;
+      case 32 * 8 + 8: e = launch_tiles_of<8, 8>(a, grid, stream); break;
+      default: e = launch_tiles_of<0, 0>(a, grid, stream); break;
     }
+    if (e != hipSuccess) return e;
   }
   return hipGetLastError();
 }
