@@ -22,7 +22,7 @@ namespace kvq {
 namespace {
 
 constexpr float kWeightBits = 10.0f;     // weights carry 2^10: small ones stay clear of binary16's subnormals
-constexpr float kMaxSlack = 4.0f;        // the running maximum is raised once it lags by more: weights stay below 2^14
+constexpr float kMaxWeight = 32768.0f;   // the running maximum is raised once a lane's 16 weights sum to more: none passes binary16's range
 constexpr int kTileTokens = 64;
 constexpr int kRowsPerWave = 32;
 
@@ -47,8 +47,8 @@ template <int B> __device__ __forceinline__ void load_key_chunk(uint32_t* w, con
     for (int i = 0; i < B; ++i) w[i] = p[i];
   }
 }
-// ... and its codes as 16 binary16 pairs in slot order, four 16-byte pieces (PIECES 2: the first or the second half, B / 2 dwords).
-template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, uint32_t one_k, u32x4 (&out)[PIECES]) {
+// ... and its codes as 16 pairs of binary16 subnormals in slot order, four 16-byte pieces (PIECES 2: the first or the second half, B / 2 dwords).
+template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, u32x4 (&out)[PIECES]) {
   constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
   constexpr int P = 16 / LO;                       // pairs per dword
   constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
@@ -67,7 +67,7 @@ template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chun
         x |= ((w[LO + at / 32] >> (at % 32)) & hmask) << LO;
         x |= ((w[LO + next / 32] >> (next % 32)) & hmask) << (LO + 16);
       }
-      out[s >> 2][s & 3] = as_u32(whole_to_half2(x, HI != 0 ? ~0u : mask, one_k));
+      out[s >> 2][s & 3] = HI != 0 ? x : x & mask;
     }
   }
 }
@@ -186,6 +186,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
   float m = kNoMax, l = 0.0f;
   const bool two_parts = g.bits_v != 16;                   // (patterns of an unquantized plane have no second part)
+  const float code_unit = g.bits_k == 16 ? 1.0f : 16777216.0f;               // key codes stand as binary16 subnormals, in units of 2^-24
   const uint32_t one_k = one_k_pattern(), v_mask = ((1u << min(g.bits_v, 15)) - 1u) * 0x00010001u;
 
   // (a block of tiles: [0, sink_tiles) and [first, ...))
@@ -197,15 +198,21 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
   const int vblk = tid / (128 * 4 / kTiles), half = (tid >> 6) & (8 / kTiles - 1), j = lane >> 4, dl = lane & 15;
   const int x_ = tok & 31, k_row = (tok & 32) | (x_ & 7) | ((x_ & 8) << 1) | ((x_ & 16) >> 1);        // bits 3 and 4 swapped
   const int per_group = g.g_v >> 4;                        // 16-channel tiles of a value group
-  auto key_source = [&](int t0, int64_t base) { return base + (min(t0 + tok, limit - 1) - t0); };      // (nothing behind the last visible token is read)
-  auto value_source = [&](int t0, int64_t base) { return (base >> 5) + (min((t0 >> 5) + vblk, (limit - 1) >> 5) - (t0 >> 5)); };
-  auto load_metas = [&](int64_t src, int64_t vsrc, bool raw_k, bool raw_v, uint32_t& km, u32x4 (&vm)[kTiles]) {
-    km = raw_k ? 0x00003C00u : ((const uint32_t*)a.cache.k_meta)[meta_index(src, min(chunk, NG - 1), NG)];                 // (unquantized: scale 1, zero 0)
+  // Addresses: where the tile begins, the same for all lanes, and a 32-bit distance from there
+  auto tile_base = [&](int t0) {
+    const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)base), hi = __builtin_amdgcn_readfirstlane((int)(base >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+  };
+  auto key_distance = [&](int t0) { return (uint32_t)min(tok, limit - 1 - t0); };              // (nothing behind the last visible token is read)
+  auto value_distance = [&](int t0) { return (uint32_t)min(vblk, (limit - 1 - t0) >> 5); };
+  auto load_metas = [&](int64_t base, uint32_t dk, uint32_t dv, bool raw_k, bool raw_v, uint32_t& km, u32x4 (&vm)[kTiles]) {
+    km = raw_k ? 0x00003C00u : ((const uint32_t*)a.cache.k_meta + base * NG)[(dk >> 4) * (16 * NG) + 16 * min(chunk, NG - 1) + (dk & 15)];                 // (unquantized: scale 1, zero 0)
     if (raw_v) return;
 #pragma unroll
     for (int n = 0; n < kTiles / 2; ++n) {
       if (n == 1 && per_group != 2) break;                 // uniform: half a row is one group, or two
-      const uint32_t* mp = (const uint32_t*)a.cache.v_meta + meta_index(32 * vsrc, (kTiles * half + 2 * n) / per_group, g.ng_v) + 4 * j;
+      const uint32_t* mp = (const uint32_t*)a.cache.v_meta + base * g.ng_v + (32 * dv * g.ng_v + 16 * (uint32_t)((kTiles * half + 2 * n) / per_group) + 4 * j);
 #pragma unroll
       for (int x4 = 0; x4 < 2; ++x4) vm[2 * n + x4] = *reinterpret_cast<const u32x4*>(mp + 16 * g.ng_v * x4);
     }
@@ -217,7 +224,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     for (int i = 0; i < kPieces; ++i)
       *reinterpret_cast<u32x4*>(sm_k + k_row * 256 + (((4 * chunk + kPieces * sub + i) ^ (k_row & 15)) << 4)) = piece[i];
     if (t0 + tok >= limit || chunk >= NG) km = 0;
-    sm_scale_[at][chunk][k_row] = widen16((uint16_t)km, false);
+    sm_scale_[at][chunk][k_row] = widen16((uint16_t)km, false) * code_unit;
     sm_zero_[at][k_row][chunk] = (km >> 16) * 0x00010001u;
 
     const int valid = limit - (t0 + 32 * vblk + 4 * j);    // of tokens 16 x4 + 4 j + r those with 16 x4 + r < valid are visible to some row
@@ -311,11 +318,35 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
           s[i] = seen ? s[i] : -INFINITY;
         }
       }
-      float most = s[0];
+      // Weights with the maximum as it stands; only if their sum shows that it lags is it raised, and they are formed again
+      u32x4 pw[2], pl[2];
+      float sum;
+      auto weights = [&]() {
+        const float off = kWeightBits - m;
+        sum = 0.0f;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
-      most = fmaxf(most, other_half(most)) * kappa;
-      if (__any(most > m + kMaxSlack)) {
+        for (int v = 0; v < 8; ++v) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * v], kappa, off)), y = __builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], kappa, off));
+          half2v p;
+          p[0] = (_Float16)x;
+          p[1] = (_Float16)y;
+          pw[v >> 2][v & 3] = as_u32(p);
+          if constexpr (FINE) {
+            sum += x + y;
+            half2v q;
+            q[0] = (_Float16)(x - (float)p[0]); q[1] = (_Float16)(y - (float)p[1]);
+            pl[v >> 2][v & 3] = as_u32(q);
+          } else {
+            sum = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+          }
+        }
+      };
+      weights();
+      if (__any(sum > kMaxWeight)) {
+        float most = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+        most = fmaxf(most, other_half(most)) * kappa;
         const float m_new = fmaxf(m, most), f = exp2f(m - m_new);
         m = m_new;
         l *= f;
@@ -323,25 +354,9 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
         for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[ct][i] *= f;
+        weights();
       }
-      const float off = kWeightBits - m;
-      u32x4 pw[2], pl[2];
-#pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * v], kappa, off)), y = __builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], kappa, off));
-        half2v p;
-        p[0] = (_Float16)x;
-        p[1] = (_Float16)y;
-        pw[v >> 2][v & 3] = as_u32(p);
-        if constexpr (FINE) {
-          l += x + y;
-          half2v q;
-          q[0] = (_Float16)(x - (float)p[0]); q[1] = (_Float16)(y - (float)p[1]);
-          pl[v >> 2][v & 3] = as_u32(q);
-        } else {
-          l = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, l, false);
-        }
-      }
+      l += sum;
       const uint8_t* vt = sm_v + blk * 8192;
 #pragma unroll
       for (int st = 0; st < 2; ++st)
@@ -363,18 +378,19 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     u32x4 raw_vm[kTiles];
     auto load = [&](int ti) {
       const int t0 = first_token(ti);
-      const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0), src = key_source(t0, base), vsrc = value_source(t0, base);
-      load_words<BK / 2>(raw_k, (const uint32_t*)a.cache.k_codes + src * (4 * BK) + chunk * BK + sub * (BK / 2));
+      const int64_t base = tile_base(t0);
+      const uint32_t dk = key_distance(t0), dv = value_distance(t0);
+      load_words<BK / 2>(raw_k, (const uint32_t*)a.cache.k_codes + base * (4 * BK) + (dk * (4 * BK) + chunk * BK + sub * (BK / 2)));
       constexpr int kWords = BV / 2;                         // of the lane's 2 BV, which lie in fours: 256 words from one four to the next
       const int w = kWords * half;
-      load_words<kWords>(raw_v, (const uint32_t*)a.cache.v_codes + vsrc * (128 * BV) + 256 * (w >> 2) + 4 * lane + (w & 3));
-      load_metas(src, vsrc, false, false, raw_km, raw_vm);
+      load_words<kWords>(raw_v, (const uint32_t*)a.cache.v_codes + base * (4 * BV) + (dv * (128 * BV) + 256 * (w >> 2) + 4 * lane + (w & 3)));
+      load_metas(base, dk, dv, false, false, raw_km, raw_vm);
     };
     // The loaded tile, to buffer `at`
     auto unpack = [&](int ti, int at) {
       u32x4 piece[kPieces];
       uint32_t f[kPairs];
-      unpack_key_chunk<BK, kPieces>(raw_k, raw_bf, one_k, piece);
+      unpack_key_chunk<BK, kPieces>(raw_k, raw_bf, piece);
       value_fields<BV, false, kPairs>(raw_v, f);
       store(piece, raw_km, f, raw_vm, false, first_token(ti), at);
     };
@@ -384,30 +400,35 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
       if (t_begin + 1 < t_end) load(t_begin + 1);
       __syncthreads();
     }
-    for (int ti = t_begin; ti < t_end; ++ti) {
-      const int at = (ti - t_begin) & 1;
+    auto step = [&](int ti, int at) {
       compute(ti, at);
       if (ti + 1 < t_end) unpack(ti + 1, 1 - at);
       if (ti + 2 < t_end) load(ti + 2);
       __syncthreads();
+    };
+    for (int ti = t_begin; ti < t_end; ti += 2) {          // (two steps a turn: `at` is a constant, addresses in LDS are)
+      step(ti, 0);
+      if (ti + 1 == t_end) break;
+      step(ti + 1, 1);
     }
   } else {
     // A tile of widths told at run time
     auto load_and_unpack = [&](int ti) {
       const int t0 = first_token(ti), bits_k = g.bits_k, bits_v = g.bits_v;
-      const int64_t base = virtual_token(g, a.cache.page_table, b, h, t0), src = key_source(t0, base), vsrc = value_source(t0, base);
-      const uint32_t* kp = (const uint32_t*)a.cache.k_codes + src * (4 * bits_k) + chunk * bits_k;
-      const uint32_t* vp = (const uint32_t*)a.cache.v_codes + vsrc * (128 * bits_v);
+      const int64_t base = tile_base(t0);
+      const uint32_t dk = key_distance(t0), dv = value_distance(t0);
+      const uint32_t* kp = (const uint32_t*)a.cache.k_codes + base * (4 * bits_k) + (dk * (4 * bits_k) + chunk * bits_k);
+      const uint32_t* vp = (const uint32_t*)a.cache.v_codes + base * (4 * bits_v) + dv * (128 * bits_v);
       u32x4 piece[4], vm[4];
       uint32_t w[16], f[16], km;
       switch (bits_k) {
-        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1>(w, raw_bf, one_k, piece); break;
-        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2>(w, raw_bf, one_k, piece); break;
-        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3>(w, raw_bf, one_k, piece); break;
-        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4>(w, raw_bf, one_k, piece); break;
-        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6>(w, raw_bf, one_k, piece); break;
-        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8>(w, raw_bf, one_k, piece); break;
-        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16>(w, raw_bf, one_k, piece); break;
+        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1>(w, raw_bf, piece); break;
+        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2>(w, raw_bf, piece); break;
+        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3>(w, raw_bf, piece); break;
+        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4>(w, raw_bf, piece); break;
+        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6>(w, raw_bf, piece); break;
+        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8>(w, raw_bf, piece); break;
+        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16>(w, raw_bf, piece); break;
       }
       switch (bits_v) {
         case 1: load_value_half<1>(w, vp, lane, half); value_fields<1>(w, f); break;
@@ -429,7 +450,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
           for (int s = 0; s < 16; ++s) f[s] |= hi[s] << lo;
         }
       }
-      load_metas(src, vsrc, bits_k == 16, bits_v == 16, km, vm);
+      load_metas(base, dk, dv, bits_k == 16, bits_v == 16, km, vm);
       store(piece, km, f, vm, bits_v == 16, t0, 0);
     };
     for (int ti = t_begin; ti < t_end; ++ti) {
