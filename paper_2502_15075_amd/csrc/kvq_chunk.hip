@@ -122,6 +122,22 @@ __device__ __forceinline__ Walk make_walk(int p_first, int p_last, int window, i
   return w;
 }
 
+// The tokens of row tile `tile` of sequence b and the parts they are cut into
+struct TileSpan { int rows, row0, p0, p_last, parts; Walk walk; };
+__device__ __forceinline__ TileSpan tile_span(const ChunkArgs& a, int b, int tile, int tile_rows) {
+  TileSpan s;
+  const int R = a.heads_per_kv;
+  const int len = a.seq_lens ? min(max(a.seq_lens[b], 0), a.seq_bound) : a.seq_bound;
+  const int nq = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
+  s.rows = nq * R;
+  s.row0 = tile * tile_rows;
+  s.p0 = len - nq;                                         // position of query token 0
+  s.p_last = s.p0 + __builtin_amdgcn_readfirstlane((min(s.row0 + tile_rows, s.rows) - 1) / R);
+  s.walk = make_walk(s.p0 + __builtin_amdgcn_readfirstlane(s.row0 / R), s.p_last, a.window, a.sinks);
+  s.parts = a.splits == 1 ? 1 : max(__builtin_amdgcn_readfirstlane((s.walk.n + a.per - 1) / a.per), 1);
+  return s;
+}
+
 constexpr int tile_waves(int bk) { return bk ? 8 : 4; }
 
 // BK, BV: the widths, or 0 and 0: any, told at run time.  With widths known a thread's share of the next tile is loaded while this one is computed,
@@ -136,24 +152,16 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
   __shared__ __attribute__((aligned(16))) uint32_t sm_zero_[kBuffers][kTileTokens][4];         // key zeros, each twice
   __shared__ __attribute__((aligned(16))) uint32_t sm_qsum[kTileRows][4];                      // group sums of the query, two parts each
   __shared__ float sm_kappa[kTileRows];
-  __shared__ int sm_last;
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // (a division leaves its result in vector registers, and with it every address: these are the same in all lanes)
   const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / g.kv_heads), h = blockIdx.x - b * g.kv_heads;
   const int R = a.heads_per_kv;
-  const int len = a.seq_lens ? min(max(a.seq_lens[b], 0), a.seq_bound) : a.seq_bound;
-  const int nq = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
-  // later rows see more: they go first
-  const int split = blockIdx.z, tile = (int)gridDim.y - 1 - (int)blockIdx.y;
-  const int row0 = tile * kTileRows, rows = nq * R;
-  if (row0 >= rows) return;
-  const int row_end = min(row0 + kTileRows, rows);
-  const int p0 = len - nq;                               // position of query token 0
-  const int p_last = p0 + __builtin_amdgcn_readfirstlane((row_end - 1) / R);
-  const Walk walk = make_walk(p0 + __builtin_amdgcn_readfirstlane(row0 / R), p_last, a.window, a.sinks);
-  const int parts = a.splits == 1 ? 1 : max(__builtin_amdgcn_readfirstlane((walk.n + a.per - 1) / a.per), 1);
-  if (split >= parts) return;                            // uniform
+  const int split = blockIdx.z, tile = (int)gridDim.y - 1 - (int)blockIdx.y;          // later rows see more: they go first
+  const TileSpan span = tile_span(a, b, tile, kTileRows);
+  const int row0 = span.row0, rows = span.rows, p0 = span.p0, p_last = span.p_last, parts = span.parts;
+  const Walk walk = span.walk;
+  if (row0 >= rows || split >= parts) return;              // uniform
   const int t_begin = split * a.per, t_end = min(t_begin + a.per, walk.n);
   const int limit = p_last + 1;                          // no row of the tile sees a token from here on
   const bool raw_bf = g.raw_dtype == KVQ_BF16;
@@ -501,21 +509,17 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
   }
   const int row = row0 + my_row;
   const int64_t hq = ((int64_t)b * a.n_q + row / R) * a.q_heads + h * R + row % R;
-  if (parts > 1) {
-    MergeWord* const word = a.words + (int64_t)tile * gridDim.x + blockIdx.x;
-    if (tid == 0) merge_announce(word, a.merge_tag);
-    if (row < rows) {
-      float* rec = a.ws + (hq * a.splits + split) * kRec;
+  if (row >= rows) return;
+  if (parts > 1) {                                         // (joined by the launch behind this one)
+    float* rec = a.ws + (hq * a.splits + split) * kRec;
 #pragma unroll
-      for (int ct = 0; ct < 4; ++ct)
+    for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) store_record2(rec + 32 * ct + 8 * (i >> 2) + 4 * hh + (i & 3), acc[ct][i], acc[ct][i + 1]);
-      if (hh == 0) store_record2(rec + kHeadDim, m, l);
-    }
-    if (merge_arrive(word, a.merge_tag, parts, tid, &sm_last)) merge_rows<64 * kWaves>(a, b, h, row0, row_end - row0, parts, tid);
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4v*>(rec + 32 * ct + 8 * q + 4 * hh) = float4v{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
+    if (hh == 0) *reinterpret_cast<float2*>(rec + kHeadDim) = make_float2(m, l);
     return;
   }
-  if (row >= rows) return;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;            // (a row that sees nothing: zeros)
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
@@ -529,47 +533,65 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     }
 }
 
+// Rows whose tokens were cut into parts, 16 a workgroup (one workgroup for all rows of a tile took 30 to 80 us for 2 to 16 parts of 256 rows)
+constexpr int kJoinRows = 16;
+__global__ __launch_bounds__(32 * kJoinRows) void join_kernel(const ChunkArgs a, int tile_rows) {
+  const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.g.kv_heads), h = blockIdx.x - b * a.g.kv_heads;
+  const int row0 = kJoinRows * blockIdx.y;
+  const TileSpan span = tile_span(a, b, __builtin_amdgcn_readfirstlane(row0 / tile_rows), tile_rows);
+  if (row0 >= span.rows || span.parts == 1) return;
+  merge_rows<32 * kJoinRows>(a, b, h, row0, min(kJoinRows, span.rows - row0), span.parts, threadIdx.x);
+}
+
 }  // namespace
 
-// Up to kFewRowsMax rows of a kv head go to the kernel that keeps the cache packed, more to the tiles above.  The tokens are cut into parts
-// where there are fewer workgroups than compute units, as long as a part leaves every wavefront a few steps.
-constexpr int kFewRowsMax = 128;
-// (the widths of every day have tiles of 256 rows, all others share the kernel without widths)
-bool tile_widths(int bk, int bv) { return (bk == 2 || bk == 4 || bk == 8) && (bv == 2 || bv == 4 || bv == 8); }
-int tile_rows(const Geom& g) { return kRowsPerWave * tile_waves(tile_widths(g.bits_k, g.bits_v) ? g.bits_k : 0); }
+// Widths 2, 4 and 8 have row tiles of 256 rows, all others share the kernel that is told them at run time, 128 rows.
+static bool tile_widths(int bk, int bv) { return (bk == 2 || bk == 4 || bk == 8) && (bv == 2 || bv == 4 || bv == 8); }
+static int tile_rows(const Geom& g) { return kRowsPerWave * tile_waves(tile_widths(g.bits_k, g.bits_v) ? g.bits_k : 0); }
+
+// What a choice costs: each workgroup `fixed` ns and `unit` ns for each of its units of tokens, in rounds of as many workgroups as the device
+// takes at once, `join` ns where parts are joined.  Measured at 4/2 bits (a call's time in us, predicted and measured):
+//   few rows, 1 column set, 256 workgroups x 130 blocks: 33, 30; cut in three 36, 41     8 workgroups x 33 blocks: 14, 14; cut in eight 11, 11
+//   few rows, 3 column sets, 48 workgroups x 256 blocks: 99, 88; cut in four 41, 39; in eight (a second round) 55, 54
+//   row tiles, 8 workgroups x 128 tiles: 314, 311             16 x 16 tiles: 57, 57      64 x 4 tiles: 29, 28
+struct ChunkCost { int64_t fixed, unit, join; };
+static void cheapest_split(const ChunkCost& c, int64_t groups, int64_t at_once, int64_t share, int64_t units, int64_t* splits, int64_t* cost) {
+  *cost = INT64_MAX;
+  for (const int64_t s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+    const int64_t n = groups * s;
+    if (s > 1 && (s > units || n > 2 * at_once)) break;
+    // (`share`: workgroups that have a compute unit's full speed between them; those beyond take turns)
+    const int64_t t = (n + at_once - 1) / at_once * c.fixed + (n + share - 1) / share * c.unit * ((units + s - 1) / s) + (s > 1 ? c.join : 0);
+    if (t < *cost) { *cost = t; *splits = s; }
+  }
+}
 ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_bound, int32_t window, int32_t sinks) {
-  ChunkPlan plan{0, 1, 1};
-  const int64_t rows = (int64_t)n_q * heads_per_kv, streams = (int64_t)g.batch * g.kv_heads;
-  // the units (blocks of 32 tokens, tiles of 64) that a row tile of so many query tokens sees at most
-  auto units_of = [&](int64_t unit, int64_t tokens) {
+  const int64_t rows = (int64_t)n_q * heads_per_kv, streams = (int64_t)g.batch * g.kv_heads, cus = device_compute_units();
+  // the units (blocks of 32 tokens, tiles of 64) that a row tile of so many rows sees at most
+  auto units_of = [&](int64_t unit, int64_t tile) {
     int64_t all = (seq_bound + unit - 1) / unit;
-    if (window && tokens > n_q) tokens = n_q;
     if (window) {
-      const int64_t some = ((int64_t)window + tokens - 1 + unit - 2) / unit + 1 + ((int64_t)sinks + unit - 1) / unit;
+      const int64_t tokens = (tile + heads_per_kv - 2) / heads_per_kv + 1;     // (a tile may begin inside a token's rows)
+      const int64_t some = ((int64_t)window + (tokens > n_q ? n_q : tokens) - 1 + unit - 2) / unit + 1 + ((int64_t)sinks + unit - 1) / unit;
       if (some < all) all = some;
     }
     return all < 1 ? 1 : all;
   };
-  int64_t splits;
-  if (rows <= kFewRowsMax) {
-    const int ngk = g.bits_k == 16 ? 1 : g.ng_k, ngv = g.bits_v == 16 ? 1 : g.ng_v;
-    const int most = few_max_sets(g.bits_k, g.bits_v, ngk > ngv ? ngk : ngv), sets = (int)((rows + 15) / 16);
-    const int tiles = (sets + most - 1) / most;
-    plan.few_sets = (sets + tiles - 1) / tiles;            // as few row tiles as can be, of the same size
-    const int64_t groups = streams * tiles;
-    const int64_t blocks = units_of(32, 16 * plan.few_sets);
-    plan.units = (int32_t)blocks;
-    splits = (plan.few_sets == 1 ? 2 : 1) * device_compute_units() / groups;
-    if (splits > blocks / 16) splits = blocks / 16;
-  } else {
-    const int at_once = tile_rows(g);
-    const int64_t tiles = (rows + at_once - 1) / at_once * streams, steps = units_of(kTileTokens, at_once);
-    plan.units = (int32_t)steps;
-    splits = (256 / at_once * device_compute_units() + tiles - 1) / tiles;
-    if (splits > steps / 4) splits = steps / 4;
-  }
-  plan.splits = (int32_t)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
-  return plan;
+  // few rows: the cache stays packed, every wavefront takes blocks of its own for up to three sets of 16 rows
+  const int ngk = g.bits_k == 16 ? 1 : g.ng_k, ngv = g.bits_v == 16 ? 1 : g.ng_v, ng = ngk > ngv ? ngk : ngv;
+  const int64_t most = few_max_sets(g.bits_k, g.bits_v, ng), sets = (rows + 15) / 16, few_tiles = (sets + most - 1) / most;
+  const int few_sets = (int)((sets + few_tiles - 1) / few_tiles);              // as few row tiles as can be, of the same size
+  const int64_t blocks = units_of(32, 16 * few_sets), resident = few_occupancy(g.bits_k, g.bits_v, few_sets, ng) / 2;
+  const ChunkCost few{3500 + 3500 * few_sets, (g.bits_k + g.bits_v > 8 ? 170 : 130) + 70 * few_sets, 2000 * few_sets};
+  int64_t few_splits = 1, few_cost;
+  cheapest_split(few, streams * few_tiles, resident * cus, cus, blocks, &few_splits, &few_cost);
+  if (few_tiles == 1) return ChunkPlan{few_sets, (int32_t)few_splits, (int32_t)blocks};      // (row tiles would be filled to less than a fifth)
+  // more rows: tiles
+  const int64_t at_once = tile_rows(g), tiles = (rows + at_once - 1) / at_once * streams, steps = units_of(kTileTokens, at_once);
+  const ChunkCost tile{20000, at_once == 256 ? 2300 : 1600, 10000};
+  int64_t tile_splits = 1, tile_cost;
+  cheapest_split(tile, tiles, 256 / at_once * cus, cus, steps, &tile_splits, &tile_cost);
+  return few_cost <= tile_cost ? ChunkPlan{few_sets, (int32_t)few_splits, (int32_t)blocks} : ChunkPlan{0, (int32_t)tile_splits, (int32_t)steps};
 }
 size_t chunk_record_bytes(int32_t batch, int32_t n_q, int32_t q_heads, int32_t splits) {
   return splits <= 1 ? 0 : (size_t)batch * n_q * q_heads * splits * kRec * sizeof(float);
@@ -604,8 +626,8 @@ hipError_t launch_few(const ChunkArgs& a, int32_t sets, hipStream_t stream) {
 
 hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, hipStream_t stream) {
   ChunkArgs a = args;
-  if (a.splits > 1) a.merge_tag = next_merge_tag();
   if (plan.few_sets) {
+    if (a.splits > 1) a.merge_tag = next_merge_tag();
     const hipError_t e = launch_few(a, plan.few_sets, stream);
     if (e != hipSuccess) return e;
   } else {
@@ -625,6 +647,10 @@ hipError_t launch_chunk_attention(const ChunkArgs& args, const ChunkPlan& plan, 
       default: e = launch_tiles_of<0, 0>(a, grid, stream); break;
     }
     if (e != hipSuccess) return e;
+    if (a.splits > 1) {
+      const dim3 joins(grid.x, (a.n_q * a.heads_per_kv + kJoinRows - 1) / kJoinRows);
+      hipLaunchKernelGGL(join_kernel, joins, dim3(32 * kJoinRows), 0, stream, a, at_once);
+    }
   }
   return hipGetLastError();
 }

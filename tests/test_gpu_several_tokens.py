@@ -4,12 +4,14 @@ Appends are held byte for byte to the CPU oracle, which is given the keys rotate
 
 Attention is held to the formula in binary64 over the rows that kvq_dequantize returns, element by element, within
 
-    (3 r + 2 delta) * sum_t p_t |V^_t|  +  r 2^-13 * sum_t |V^_t| / l  +  half a step of the output type,   l = sum_t p_t / p_max,
+    (3 r + 2 delta) * sum_t p_t |V^_t|  +  r / 2 * sum_t p_t (V^_t - min V^_t)  +  r 2^-13 * sum_t |V^_t| / l  +  half a step of the output type,
 
-with r = 2^-11 for 16-bit outputs and 2^-21 for binary32 ones.  16-bit outputs: the kernels round every reconstructed value (or its weight,
+l = sum_t p_t / p_max, with r = 2^-11 for 16-bit outputs and 2^-21 for binary32 ones.  16-bit outputs: the kernels round every reconstructed value (or its weight,
 scale included) and every weight once to binary16, half a step 2^-11 of it each, and the weights' sum may follow the rounded weights or not
 (numerator and denominator: one more).  Binary32 outputs: weights and values travel as two binary16 parts, so that 2^-22 of each is lost, and the
-products are summed in binary32.  Weights far below a row's largest fall among binary16's subnormals: their step there is 2^-24 of a largest weight of
+products are summed in binary32.  A weight that is rounded with its scale meets the code: the error is relative to p_t scale code, not to V^_t, which
+is zero + scale code and may be much smaller where the two cancel.  scale code = V^_t less the least V^ of its token and group, whose code is 0; the
+rounded product p_t scale is off by half a step, r / 2 of it.  Weights far below a row's largest fall among binary16's subnormals: their step there is 2^-24 of a largest weight of
 at least 2^8, as are the steps of second parts.  delta is what the logits may be off by: 130 binary32 additions and the roundings of scale and
 exponent, 2^-24 each, of sums whose terms are bounded by sum_d |q_d| times the greatest |K^| (twice: codes and zeros are summed apart).
 """
@@ -96,6 +98,8 @@ def _reference(kvq, oracle, L, cache, q, q_lens, seq_lens, window, sinks, scale,
     R = Hq // L.kv_heads
     T = max(1, max(seq_lens))
     K, V = _dequantized(kvq, L, cache, T)
+    groups = V.view(*V.shape[:3], -1, L.group_v)
+    lift = (groups - groups.amin(-1, keepdim=True)).reshape(V.shape) if L.bits_v != 16 else torch.zeros_like(V)
     qd = q.double().cuda()
     if L.rotate_k:                                     # the library's rotated query is rounded to binary16
         x = q.float().cpu().numpy().reshape(-1, 128)
@@ -128,7 +132,7 @@ def _reference(kvq, oracle, L, cache, q, q_lens, seq_lens, window, sinks, scale,
                 mag = w @ v.abs() / l
                 delta = 2 * 132 * 2.0 ** -24 * scale * x.abs().sum(-1, keepdim=True) * k.abs().amax() / 2
                 r = 2.0 ** -21 if out_dtype == torch.float32 else 2.0 ** -11
-                tol[b, :n, hq] = (3 * r + 2 * delta) * mag + r * 2.0 ** -13 * (seen.double() @ v.abs()) / l
+                tol[b, :n, hq] = (3 * r + 2 * delta) * mag + r / 2 * (w @ lift[b, h, :length] / l) + r * 2.0 ** -13 * (seen.double() @ v.abs()) / l
     tol += HALF_STEP[out_dtype] * want.abs().nan_to_num()
     return want, tol
 
