@@ -554,14 +554,15 @@ static int tile_rows(const Geom& g) { return kRowsPerWave * tile_waves(tile_widt
 //   few rows, 1 column set, 256 workgroups x 130 blocks: 33, 30; cut in three 36, 41     8 workgroups x 33 blocks: 14, 14; cut in eight 11, 11
 //   few rows, 3 column sets, 48 workgroups x 256 blocks: 99, 88; cut in four 41, 39; in eight (a second round) 55, 54
 //   row tiles, 8 workgroups x 128 tiles: 314, 311             16 x 16 tiles: 57, 57      64 x 4 tiles: 29, 28
-struct ChunkCost { int64_t fixed, unit, join; };
+struct ChunkCost { int64_t fixed, unit, step, join; };     // step: units that a workgroup takes at a time
 static void cheapest_split(const ChunkCost& c, int64_t groups, int64_t at_once, int64_t share, int64_t units, int64_t* splits, int64_t* cost) {
   *cost = INT64_MAX;
   for (const int64_t s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
     const int64_t n = groups * s;
     if (s > 1 && (s > units || n > 2 * at_once)) break;
     // (`share`: workgroups that have a compute unit's full speed between them; those beyond take turns)
-    const int64_t t = (n + at_once - 1) / at_once * c.fixed + (n + share - 1) / share * c.unit * ((units + s - 1) / s) + (s > 1 ? c.join : 0);
+    const int64_t t = (n + at_once - 1) / at_once * c.fixed + (n + share - 1) / share * c.unit * (((units + s - 1) / s + c.step - 1) / c.step * c.step) +
+                      (s > 1 ? c.join : 0);
     if (t < *cost) { *cost = t; *splits = s; }
   }
 }
@@ -582,13 +583,13 @@ ChunkPlan plan_chunk(const Geom& g, int heads_per_kv, int32_t n_q, int32_t seq_b
   const int64_t most = few_max_sets(g.bits_k, g.bits_v, ng), sets = (rows + 15) / 16, few_tiles = (sets + most - 1) / most;
   const int few_sets = (int)((sets + few_tiles - 1) / few_tiles);              // as few row tiles as can be, of the same size
   const int64_t blocks = units_of(32, 16 * few_sets), resident = few_occupancy(g.bits_k, g.bits_v, few_sets, ng) / 2;
-  const ChunkCost few{3500 + 3500 * few_sets, (g.bits_k + g.bits_v > 8 ? 170 : 130) + 70 * few_sets, 2000 * few_sets};
+  const ChunkCost few{3500 + 3500 * few_sets, (g.bits_k + g.bits_v > 8 ? 170 : 130) + 70 * few_sets, kFewWaves, 2000 * few_sets};
   int64_t few_splits = 1, few_cost;
   cheapest_split(few, streams * few_tiles, resident * cus, cus, blocks, &few_splits, &few_cost);
   if (few_tiles == 1) return ChunkPlan{few_sets, (int32_t)few_splits, (int32_t)blocks};      // (row tiles would be filled to less than a fifth)
   // more rows: tiles
   const int64_t at_once = tile_rows(g), tiles = (rows + at_once - 1) / at_once * streams, steps = units_of(kTileTokens, at_once);
-  const ChunkCost tile{20000, at_once == 256 ? 2300 : 1600, 10000};
+  const ChunkCost tile{20000, at_once == 256 ? 2300 : 1600, 1, 10000};
   int64_t tile_splits = 1, tile_cost;
   cheapest_split(tile, tiles, 256 / at_once * cus, cus, steps, &tile_splits, &tile_cost);
   return few_cost <= tile_cost ? ChunkPlan{few_sets, (int32_t)few_splits, (int32_t)blocks} : ChunkPlan{0, (int32_t)tile_splits, (int32_t)steps};
