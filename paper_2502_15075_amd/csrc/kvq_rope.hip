@@ -140,6 +140,18 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const RopeArgs a) {
     const int64_t src = row0 + i * a.st;
     const uint4 kraw = *reinterpret_cast<const uint4*>(a.k_new + src + d0), kother = *reinterpret_cast<const uint4*>(a.k_new + src + other);
     const uint4 vraw = *reinterpret_cast<const uint4*>(a.v_new + src + d0);
+    // query heads two at a time, the next two on their way while two are rotated (a last one of an odd number is loaded twice, stored once)
+    const int64_t qs = b * a.q_sb + i * a.q_st + (int64_t)h * a.heads_per_kv * a.q_sh;
+    uint4 own[2], oth[2];
+    auto load_heads = [&](int r) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint16_t* const q = a.q + qs + min(r + k, a.heads_per_kv - 1) * a.q_sh;
+        own[k] = *reinterpret_cast<const uint4*>(q + d0);
+        if (!a.interleaved) oth[k] = *reinterpret_cast<const uint4*>(q + other);
+      }
+    };
+    if (a.heads_per_kv > 0) load_heads(0);         // (0: the call has no queries)
     float x[8];
     widen8<BF>(kraw, x);
     turn8<BF>(a, t, x, kother, d0);
@@ -155,12 +167,18 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const RopeArgs a) {
       case 8: stage_value_row<8, kRopeSpan>(vstage, row, d0, codes); break;
       default: stage_value_row<16, kRopeSpan>(vstage, row, d0, codes); break;
     }
-    for (int r = 0; r < a.heads_per_kv; ++r) {
-      const int hq = h * a.heads_per_kv + r;
-      const int64_t qs = b * a.q_sb + i * a.q_st + hq * a.q_sh;
-      widen8<BF>(*reinterpret_cast<const uint4*>(a.q + qs + d0), x);
-      turn8<BF>(a, t, x, *reinterpret_cast<const uint4*>(a.q + qs + other), d0);
-      *reinterpret_cast<uint4*>(a.q_out + (((int64_t)b * a.n_new + i) * a.q_heads + hq) * kHeadDim + d0) = narrow8<BF>(x);
+    uint16_t* const out = a.q_out + (((int64_t)b * a.n_new + i) * a.q_heads + (int64_t)h * a.heads_per_kv) * kHeadDim + d0;
+    for (int r = 0; r < a.heads_per_kv; r += 2) {
+      uint4 y[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        widen8<BF>(own[k], x);
+        turn8<BF>(a, t, x, oth[k], d0);
+        y[k] = narrow8<BF>(x);
+      }
+      if (r + 2 < a.heads_per_kv) load_heads(r + 2);
+      *reinterpret_cast<uint4*>(out + r * kHeadDim) = y[0];
+      if (r + 1 < a.heads_per_kv) *reinterpret_cast<uint4*>(out + (r + 1) * kHeadDim) = y[1];
     }
   }
   __syncthreads();
