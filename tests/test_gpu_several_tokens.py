@@ -452,8 +452,8 @@ def test_strided_queries(kvq, oracle):
     _assert_close(_run_chunk(kvq, L, cache, swapped, None, None, 0, 0), want, tol)
 
 
-# Calls of many rows run as tiles of 256 rows (widths 2, 4 and 8) or 128: 100 query tokens of 8 query heads in 16 streams are more workgroups of the
-# kernel for few rows than the device takes at once.
+# Calls of many rows run as tiles of 256 rows (widths 2, 4 and 8) or 128: 200 query tokens of 8 query heads in 16 streams are several times the
+# workgroups of the kernel for few rows that the device takes at once.
 
 TILE_FORMATS = [(k, v, *g) for (k, v), g in zip([(k, v) for k in (2, 4, 8) for v in (2, 4, 8)],
                                                 [(32, 64), (64, 32), (128, 128), (64, 64), (32, 32), (128, 64), (64, 128), (128, 32), (32, 128)])]
@@ -463,11 +463,11 @@ TILE_FORMATS += [(1, 1, 64, 64), (3, 6, 32, 128), (6, 3, 64, 32), (16, 16, 64, 6
 @pytest.mark.parametrize("fmt", TILE_FORMATS)
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.float16, torch.bfloat16])
 def test_row_tiles_formats(kvq, oracle, fmt, out_dtype):
-    B, H, R, T, n = 4, 4, 8, 333, 100
+    B, H, R, T, n = 4, 4, 8, 333, 200
     page = 64 * (fmt[0] % 3)
     dtype = torch.float16 if out_dtype == torch.float16 else torch.bfloat16
     L = _layout(kvq, B, H, T, *fmt, dtype=dtype, page=page)
-    lens, q_lens = [333, 100, 130, 257], [100, 100, 63, 1]
+    lens, q_lens = [333, 200, 130, 257], [200, 200, 63, 1]
     cache = _filled(kvq, L, dtype, sum(fmt), H * R, lens)
     q = _queries(51, B, n, H * R, dtype)
     out = _run_chunk(kvq, L, cache, q, q_lens, lens, 0, 0, out_dtype=out_dtype)
@@ -480,7 +480,7 @@ def test_row_tiles_formats(kvq, oracle, fmt, out_dtype):
 @pytest.mark.parametrize("R", [3, 8])
 @pytest.mark.parametrize("bits", [(4, 4), (6, 6)])
 def test_row_tiles_windows(kvq, oracle, window, sinks, R, bits):
-    B, H, T, n = 4, 4, 500, 290 if R == 3 else 110
+    B, H, T, n = 4, 4, 500, 480 if R == 3 else 220
     L = _layout(kvq, B, H, T, *bits, page=128)
     lens = [500, 333, n, n - 37]                          # (the last one: rows that see nothing)
     cache = _filled(kvq, L, torch.float16, 52, H * R, lens)
@@ -494,7 +494,7 @@ def test_row_tiles_windows(kvq, oracle, window, sinks, R, bits):
 @pytest.mark.parametrize("rot", [(1, 0), (1, 1), (0, 1)])
 @pytest.mark.parametrize("fmt", [(4, 4, 64, 64), (8, 2, 32, 128), (3, 3, 64, 64)])
 def test_row_tiles_rotated_basis(kvq, oracle, rot, fmt):
-    B, H, R, T, n = 4, 4, 8, 150, 100
+    B, H, R, T, n = 4, 4, 8, 250, 200
     L = _layout(kvq, B, H, T, *fmt, rot=rot[0], rotv=rot[1])
     cache = _filled(kvq, L, torch.float16, 54, H * R)
     q = _queries(55, B, n, H * R, torch.float16)
@@ -510,9 +510,9 @@ def test_row_tiles_rotated_basis(kvq, oracle, rot, fmt):
 def test_row_tiles_in_parts(kvq, oracle, fmt, window, sinks):
     """Many rows of few sequences: parts, joined by a launch of their own; query tokens of sequences of different lengths see different
     numbers of parts, some rows none of them and some a single one."""
-    B, H, R, T, n = 3, 1, 8, 6000, 400
+    B, H, R, T, n = 3, 1, 8, 6000, 700
     L = _layout(kvq, B, H, T, *fmt)
-    lens, q_lens = [6000, 700, 120], [400, 400, 130]
+    lens, q_lens = [6000, 800, 120], [700, 700, 130]
     cache = _filled(kvq, L, torch.bfloat16, 56, H * R, lens)
     q = _queries(57, B, n, H * R, torch.bfloat16)
     want, tol = _reference(kvq, oracle, L, cache, q, q_lens, lens, window, sinks, SCALE, torch.bfloat16)
@@ -525,7 +525,7 @@ def test_row_tiles_in_parts(kvq, oracle, fmt, window, sinks):
 def test_row_tiles_scores_that_climb(kvq, oracle):
     """Each later token scores higher, by far more than a weight may hold: the running maximum is raised again and again.  And one sequence
     whose first token is the largest by as much."""
-    B, H, R, T, n = 4, 4, 8, 400, 100
+    B, H, R, T, n = 4, 4, 8, 400, 200
     L = _layout(kvq, B, H, T, 8, 4)
     g = torch.Generator().manual_seed(58)
     K = torch.randn(B, H, T, 128, generator=g)
