@@ -321,14 +321,16 @@ kvq_status kvq_rope_append(const kvq_layout* layout, const kvq_cache* cache, con
  *   window == 0, or t > p - window, or t < sinks:
  * all of them, or the newest `window` (its own among them) and the first `sinks`.  A query with p < 0 sees nothing; its output is 0.
  *   q              [B][n_q][q_heads][D], KVQ_F16 or KVQ_BF16, element strides given, D contiguous, 16-byte aligned rows (bfloat16 is
- *                  converted to binary16: values beyond its range are not supported, those below 2^-14 lose bits).
+ *                  converted to binary16: values beyond its range are not supported, those below 2^-14 lose bits; elements below 2^-27 of
+ *                  their row's largest may count as zeros).
  *   q_lens         device, int32[B], clamped to [0, n_q]; NULL: n_q each.  Rows of `out` from q_lens[b] on stay as they are.
  *   seq_lens       device, int32[B], clamped to [0, max_seq_len]; NULL: max_seq_len each.
  *   out            [B][n_q][q_heads][D] contiguous, KVQ_F32, KVQ_F16 or KVQ_BF16 (rounded once).
  *   workspace      kvq_chunk_workspace_bytes(layout, q_heads, n_q, max_seq_len, window, sinks) bytes, 16-byte aligned; with fewer (or
  *                  NULL) the tokens are cut into fewer parts, which is slower, and rounds differently.  What it holds before a call does
- *                  not matter; calls that overlap in time need one each.
- * n_q == 0 is a no-op.  Values that a cache holds in places no query sees (behind a sequence's end, in unused pages) are never used. */
+ *                  not matter; calls that overlap in time need one each, a captured call whenever its graph may run.
+ * n_q == 0 is a no-op.  What a cache holds for tokens that no query of the call sees (behind a sequence's end, older than every
+ * window, in unused pages) is never used. */
 kvq_status kvq_chunk_workspace_bytes(const kvq_layout* layout, int32_t q_heads, int32_t n_q, int32_t max_seq_len, int32_t window,
                                      int32_t sinks, size_t* bytes_out);
 kvq_status kvq_chunk_attention(const kvq_layout* layout, const kvq_cache* cache, const void* q, kvq_dtype q_dtype, int32_t q_heads,

@@ -320,6 +320,11 @@ namespace {
 kvq_status several_tokens_supported(const kvq_layout* L) {
   return kvq::has_residual(*L) ? KVQ_ERR_UNSUPPORTED : KVQ_OK;
 }
+// A window that reaches past the longest sequence is none, and no more sinks count than it has tokens (sums with them stay in 32 bits).
+void clamp_window(int32_t max_seq_len, int32_t* window, int32_t* sinks) {
+  if (*window >= max_seq_len) *window = 0;
+  if (*sinks > max_seq_len) *sinks = max_seq_len;
+}
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 kvq_status chunk_check(const kvq_layout* L, int32_t q_heads, int32_t n_q, int32_t max_seq_len, int32_t window, int32_t sinks) {
@@ -355,6 +360,7 @@ kvq_status chunk_common(const kvq_layout* layout, const kvq_cache* cache, const 
   a.q_sb = q_stride_b; a.q_st = q_stride_t; a.q_sh = q_stride_h;
   a.q_heads = q_heads; a.heads_per_kv = q_heads / layout->kv_heads; a.n_q = n_q;
   a.q_lens = q_lens; a.seq_lens = seq_lens; a.seq_bound = max_seq_len;
+  clamp_window(max_seq_len, &window, &sinks);
   a.window = window; a.sinks = sinks; a.softmax_scale = softmax_scale;
   a.out = out; a.out_dtype = out_dtype;
   a.ws = (float*)workspace;
@@ -379,6 +385,7 @@ kvq_status kvq_chunk_workspace_bytes(const kvq_layout* layout, int32_t q_heads, 
   if (n_q == 0) return KVQ_OK;
   const kvq::Geom g = kvq::make_geom(*layout);
   const int heads = q_heads / layout->kv_heads;
+  clamp_window(max_seq_len, &window, &sinks);
   const size_t records = kvq::chunk_record_bytes(layout->batch, n_q, q_heads, kvq::plan_chunk(g, heads, n_q, max_seq_len, window, sinks).splits);
   if (records) *bytes_out = records + kvq::chunk_counter_bytes(g, heads, n_q);
   return KVQ_OK;

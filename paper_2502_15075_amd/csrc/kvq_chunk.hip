@@ -10,11 +10,19 @@
 // wants them.  Tokens reach the matrix rows with bits 3 and 4 of their number swapped, which makes the packed value blocks' order the
 // operand's order.
 //
-// A tile of 64 tokens is unpacked once per workgroup into LDS: keys as binary16 codes (0 .. 255: exact, so their products with the
-// query are too), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are rounded alike).  For outputs in
-// binary32 (FINE) weights and values travel as two binary16 parts each, 2^-22 of them, and three products are summed.  Key scales
-// are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the query's
-// group sums, each split into two binary16 parts.
+// A tile of 64 tokens is unpacked once per workgroup into LDS: keys as codes (binary16 subnormals, a whole number times a
+// power of two that the scale takes back), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are
+// rounded alike).  For outputs in binary32 (FINE) weights and values travel as two binary16 parts each, 2^-22 of them, and three products are
+// summed.  Key scales are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the
+// query's group sums, each split into two binary16 parts.
+//
+// Bound by instruction issue and by power: of a wavefront's tile (34 matrix instructions of 32 cycles) the vector instructions, unpacking's share
+// included, take about 1300 cycles beside 1088; matrix instructions of ordinary operands alone run at 20 ns each under sustained load, 14 with zeros.
+// 2048 query tokens of 32 heads on 32768 tokens, 4/2 bits: 1.06 TFLOP in 1253 us (850 TFLOP/s; a product of 8192^3 reaches 1313).  What each
+// step gave there: 128 rows a workgroup, two of them a compute unit, each tile loaded when its turn came 1640; the next tile's words on
+// their way meanwhile 1577; 256 rows, so that unpacking is shared by eight wavefronts 1419; subnormal codes, uniform addresses and a maximum
+// that is looked for only when a sum shows that it lags 1380 on one card, 1253 to 1285 on others.  Steps of four matrix instructions with the next
+// operands read ahead and the last scores' arithmetic between them, in one wavefront's code, took 30 % more vector instructions and 1685 us.
 #include "kvq_attend.h"
 #include "kvq_few.h"
 
@@ -48,9 +56,10 @@ template <int B> __device__ __forceinline__ void load_key_chunk(uint32_t* w, con
   }
 }
 // ... and its codes as 16 pairs of binary16 subnormals in slot order, four 16-byte pieces (PIECES 2: the first or the second half, B / 2 dwords).
-template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, u32x4 (&out)[PIECES]) {
+template <int B, bool FINE, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, u32x4 (&out)[PIECES]) {
   constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
   constexpr int P = 16 / LO;                       // pairs per dword
+  constexpr int base = B == 16 ? 0 : code_base<B, FINE>();
   constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
 #pragma unroll
   for (int s = 0; s < 4 * PIECES; ++s) {
@@ -67,7 +76,8 @@ template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chun
         x |= ((w[LO + at / 32] >> (at % 32)) & hmask) << LO;
         x |= ((w[LO + next / 32] >> (next % 32)) & hmask) << (LO + 16);
       }
-      out[s >> 2][s & 3] = HI != 0 ? x : x & mask;
+      if constexpr (HI != 0) out[s >> 2][s & 3] = x << base;
+      else out[s >> 2][s & 3] = (LO * f >= base ? w[dw] >> (LO * f - base) : w[dw] << (base - LO * f)) & (mask << base);
     }
   }
 }
@@ -112,11 +122,11 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t* w, const u
 }
 
 // What a workgroup walks: tokens [0, sink_tiles * 64) and [first * 64, ...), n tiles in all.
-struct Walk { int sink_tiles, first, n; };
+struct Walk { int lo, sink_tiles, first, n; };              // lo: the oldest token that a window leaves to some row
 __device__ __forceinline__ Walk make_walk(int p_first, int p_last, int window, int sinks) {
   Walk w;
-  const int lo = window ? max(p_first - window + 1, 0) : 0;
-  w.first = lo / kTileTokens;
+  w.lo = window ? max(p_first - window + 1, 0) : 0;
+  w.first = w.lo / kTileTokens;
   w.sink_tiles = min((sinks + kTileTokens - 1) / kTileTokens, w.first);
   w.n = p_last < 0 ? 0 : w.sink_tiles + (p_last / kTileTokens + 1 - w.first);
   return w;
@@ -140,8 +150,8 @@ __device__ __forceinline__ TileSpan tile_span(const ChunkArgs& a, int b, int til
 
 constexpr int tile_waves(int bk) { return bk ? 8 : 4; }
 
-// BK, BV: the widths, or 0 and 0: any, told at run time.  With widths known a thread's share of the next tile is loaded while this one is computed,
-// and 16-bit outputs have two tiles in LDS, one computed while the other is unpacked (binary32 ones, half as many again, one).
+// BK, BV: the widths, or 0 and 0: any, told at run time.  With widths known eight wavefronts take 256 rows, a thread's share of the next tile is
+// loaded while this one is computed, and there are two tiles in LDS, one computed while the other is unpacked.
 template <int BK, int BV, int NG, bool FINE>
 __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const ChunkArgs a) {
   constexpr bool kAhead = BK != 0;
@@ -194,7 +204,19 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
   float m = kNoMax, l = 0.0f;
   const bool two_parts = g.bits_v != 16;                   // (patterns of an unquantized plane have no second part)
-  const float code_unit = g.bits_k == 16 ? 1.0f : 16777216.0f;               // key codes stand as binary16 subnormals, in units of 2^-24
+  // key codes stand as binary16 subnormals; this takes them back to whole numbers
+  auto unit_of = [&]() -> float {
+    switch (kAhead ? BK : g.bits_k) {
+      case 1: return 1.0f / code_unit<1, FINE>();
+      case 2: return 1.0f / code_unit<2, FINE>();
+      case 3: return 1.0f / code_unit<3, FINE>();
+      case 4: return 1.0f / code_unit<4, FINE>();
+      case 6: return 1.0f / code_unit<6, FINE>();
+      case 8: return 1.0f / code_unit<8, FINE>();
+    }
+    return 1.0f;
+  };
+  const float from_codes = unit_of();
   const uint32_t one_k = one_k_pattern(), v_mask = ((1u << min(g.bits_v, 15)) - 1u) * 0x00010001u;
 
   // (a block of tiles: [0, sink_tiles) and [first, ...))
@@ -212,6 +234,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     const uint32_t lo = __builtin_amdgcn_readfirstlane((int)base), hi = __builtin_amdgcn_readfirstlane((int)(base >> 32));
     return (int64_t)(((uint64_t)hi << 32) | lo);
   };
+  auto seen_by_some = [&](int t) { return (t < limit) & ((t >= walk.lo) | (t < a.sinks)); };
   auto key_distance = [&](int t0) { return (uint32_t)min(tok, limit - 1 - t0); };              // (nothing behind the last visible token is read)
   auto value_distance = [&](int t0) { return (uint32_t)min(vblk, (limit - 1 - t0) >> 5); };
   auto load_metas = [&](int64_t base, uint32_t dk, uint32_t dv, bool raw_k, bool raw_v, uint32_t& km, u32x4 (&vm)[kTiles]) {
@@ -231,27 +254,27 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
       *reinterpret_cast<u32x4*>(sm_k + k_row * 256 + (((4 * chunk + kPieces * sub + i) ^ (k_row & 15)) << 4)) = piece[i];
-    if (t0 + tok >= limit || chunk >= NG) km = 0;
-    sm_scale_[at][chunk][k_row] = widen16((uint16_t)km, false) * code_unit;
+    if (!seen_by_some(t0 + tok) || chunk >= NG) km = 0;
+    sm_scale_[at][chunk][k_row] = widen16((uint16_t)km, false) * from_codes;
     sm_zero_[at][k_row][chunk] = (km >> 16) * 0x00010001u;
 
-    const int valid = limit - (t0 + 32 * vblk + 4 * j);    // of tokens 16 x4 + 4 j + r those with 16 x4 + r < valid are visible to some row
+    const int tv = t0 + 32 * vblk + 4 * j;                 // the lane's tokens: tv + 16 x4 + r
+    const bool cut = t0 + kTileTokens > limit || t0 < walk.lo;                 // uniform: some of the tile's tokens no row sees
     if (raw_v) {
 #pragma unroll
       for (int s = 0; s < kPairs; ++s) {
-        const int token = 16 * ((s & 2) >> 1) + 2 * (s & 1);       // pair v = s % 4: tokens 2 v, 2 v + 1 of the eight (x4, r)
+        const int token = tv + 16 * ((s & 2) >> 1) + 2 * (s & 1);  // pair v = s % 4: tokens 2 v, 2 v + 1 of the eight (x4, r)
         uint32_t x = raw_to_half2(f[s], raw_bf);
-        if (token >= valid) x &= 0xFFFF0000u;
-        if (token + 1 >= valid) x &= 0x0000FFFFu;
+        if (cut) x &= (seen_by_some(token) ? 0x0000FFFFu : 0u) | (seen_by_some(token + 1) ? 0xFFFF0000u : 0u);
         f[s] = x;
       }
     } else {
-      if (t0 + kTileTokens > limit) {                      // uniform: the last tile (what lies behind the end is no number)
+      if (cut) {                                           // (what a cache holds there need be no number)
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (16 * (i & 1) + r >= valid) vm[i][r] = 0u;
+            vm[i][r] = seen_by_some(tv + 16 * (i & 1) + r) ? vm[i][r] : 0u;
       }
       half2v sc[4], ze[4];                                 // scales and zeros of the four pairs
 #pragma unroll
@@ -398,7 +421,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     auto unpack = [&](int ti, int at) {
       u32x4 piece[kPieces];
       uint32_t f[kPairs];
-      unpack_key_chunk<BK, kPieces>(raw_k, raw_bf, piece);
+      unpack_key_chunk<BK, FINE, kPieces>(raw_k, raw_bf, piece);
       value_fields<BV, false, kPairs>(raw_v, f);
       store(piece, raw_km, f, raw_vm, false, first_token(ti), at);
     };
@@ -430,13 +453,13 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
       u32x4 piece[4], vm[4];
       uint32_t w[16], f[16], km;
       switch (bits_k) {
-        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1>(w, raw_bf, piece); break;
-        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2>(w, raw_bf, piece); break;
-        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3>(w, raw_bf, piece); break;
-        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4>(w, raw_bf, piece); break;
-        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6>(w, raw_bf, piece); break;
-        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8>(w, raw_bf, piece); break;
-        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16>(w, raw_bf, piece); break;
+        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1, FINE>(w, raw_bf, piece); break;
+        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2, FINE>(w, raw_bf, piece); break;
+        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3, FINE>(w, raw_bf, piece); break;
+        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4, FINE>(w, raw_bf, piece); break;
+        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6, FINE>(w, raw_bf, piece); break;
+        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8, FINE>(w, raw_bf, piece); break;
+        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16, FINE>(w, raw_bf, piece); break;
       }
       switch (bits_v) {
         case 1: load_value_half<1>(w, vp, lane, half); value_fields<1>(w, f); break;

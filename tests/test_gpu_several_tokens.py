@@ -542,6 +542,42 @@ def test_row_tiles_scores_that_climb(kvq, oracle):
         _assert_close(out, want, tol)
 
 
+@pytest.mark.parametrize("fmt", [(4, 2, 64, 64), (8, 8, 32, 32), (16, 16, 64, 64), (6, 3, 64, 32), (4, 16, 64, 64)])
+@pytest.mark.parametrize("B,H,R,n", [(1, 1, 4, 1), (3, 2, 8, 6), (4, 4, 8, 200)])
+def test_tokens_that_no_query_sees_need_be_no_numbers(kvq, fmt, B, H, R, n):
+    """NaN and infinite tokens between the sinks and the oldest window, in the blocks where those begin and end: not a bit changes."""
+    T, window, sinks = 500, 101, 5
+    L = _layout(kvq, B, H, T, *fmt)
+    g = torch.Generator().manual_seed(60)
+    K, V = (torch.randn(B, H, T, 128, generator=g).half() for _ in range(2))
+    q = _queries(61, B, n, H * R, torch.float16)
+    outs = []
+    for bad in (None, float("nan"), float("inf")):
+        k, v = K.clone(), V.clone()
+        if bad is not None:
+            k[:, :, sinks:T - n - window + 1], v[:, :, sinks:T - n - window + 1] = bad, bad
+        cache = _cache(kvq, L, 0xFF)
+        kvq.quantize_append(L, cache, k.cuda(), v.cuda(), 0)
+        cache.v_scale_exp.zero_()                         # (grows with any finite scale that was stored: no part of this)
+        for out_dtype in (torch.float32, torch.float16):
+            outs.append((out_dtype, _run_chunk(kvq, L, cache, q, None, None, window, sinks, out_dtype=out_dtype)))
+    for dtype, out in outs:
+        assert bool(out.isfinite().all())
+        assert torch.equal(out, next(o for t, o in outs if t == dtype))
+
+
+def test_the_largest_windows_and_sinks(kvq):
+    """2^31 - 1 of either, with rows before the first token: the same as no window."""
+    L = _layout(kvq, 3, 2, 200, 4, 2)
+    lens = [200, 3, 0]
+    cache = _filled(kvq, L, torch.float16, 62, 8, lens)
+    q = _queries(63, 3, 9, 8, torch.float16)
+    want = _run_chunk(kvq, L, cache, q, None, lens, 0, 0)
+    huge = 2 ** 31 - 1
+    for window, sinks in ((huge, 0), (huge, huge), (0, huge), (7, huge), (200, 3)):
+        assert torch.equal(_run_chunk(kvq, L, cache, q, None, lens, window, sinks), want)
+
+
 # ------------------------------------------------------------------------------------------------------ single tokens, a window
 
 def _run_window(kvq, L, cache, q, seq_lens, window, sinks, out_dtype=torch.float32, bound=None, workspace=True):
