@@ -127,6 +127,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const RopeArgs a) {
   const int pos = a.pos[b];
   const int count = a.n_tokens ? min(max(a.n_tokens[b], 0), a.n_new) : a.n_new;
   const int first = max(pos, 0), end = (int)min((int64_t)pos + count, (int64_t)a.capacity);    // positions that are stored
+  if (first >= end) return;                        // uniform (nothing to store; also keeps positions near 2^31 out of what follows)
   const int blk = first / kRopeSpan + blockIdx.x;
   const int lo = max(first - blk * kRopeSpan, 0), hi = min(end - blk * kRopeSpan, kRopeSpan);
   if (lo >= hi) return;                            // uniform
