@@ -7,7 +7,8 @@
 // number, a check that does not hold, the first call in a process) it returns None without having done anything, and kvq.py goes on
 // as if it were not there, so that what is refused, and how, is said in one place.
 // Host time per call through kvq.py, without and with it: a 2048-token append of one sequence 5.6 and 3.9 us (4.0 of them the
-// library and the launch, by ctypes with everything at hand), a fused step 6.7 and 4.1; back to back that append takes 5.7 and 4.5 us.
+// library and the launch, by ctypes with everything at hand), a fused step 6.7 and 4.1; back to back that append takes 5.7 and 4.5 us.  An append of one token with rotation, whose kernel takes 4.4 us:
+// 8.0 and 4.4 us back to back.
 #include <Python.h>
 #include <string.h>
 #include <unistd.h>
@@ -32,6 +33,9 @@ decltype(&kvq_decode_attention) g_attention = nullptr;
 decltype(&kvq_decode_attention_varlen) g_attention_varlen = nullptr;
 decltype(&kvq_decode_step) g_step = nullptr;
 decltype(&kvq_decode_step_varlen) g_step_varlen = nullptr;
+decltype(&kvq_rope_append) g_rope_append = nullptr;
+decltype(&kvq_chunk_attention) g_chunk = nullptr;
+decltype(&kvq_window_attention) g_window = nullptr;
 pid_t g_pid = 0;
 
 PyObject* g_layout_attr = nullptr;                 // "_c", "_struct": where kvq.py's objects keep their C structs
@@ -39,6 +43,7 @@ PyObject* g_cache_attr = nullptr;
 PyObject* g_c = nullptr;                           // "c": the method that builds them
 PyObject* g_layout_class = nullptr;                // kvq.py's Layout and Cache (bind)
 PyObject* g_cache_class = nullptr;
+PyObject* g_rope_class = nullptr;                  // ... and its Rope (bind_several)
 
 // Copies the C struct of `obj` to `to`; false where there is none.  An object of kvq.py's own class keeps its struct under `attr`; where
 // nothing is kept yet, and for any other class, which may build it in its own way, it is what obj.c() returns.  A copy, made with
@@ -133,6 +138,8 @@ const int32_t* lengths(Reader& r, PyObject* o) {
   if (!r.ok || !r.need(t->scalar_type() == at::kInt && t->is_contiguous() && t->numel() == r.layout.batch)) return nullptr;
   return static_cast<const int32_t*>(t->data_ptr());
 }
+
+const int32_t* lengths_or_none(Reader& r, PyObject* o) { return o == Py_None ? nullptr : lengths(r, o); }
 
 // What `body` returns (the library's status, or a negative number for a case that is not plain) as Python has it.
 template <typename F> PyObject* plain(F body) {
@@ -237,6 +244,82 @@ PyObject* decode_step_varlen(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (layout, cache, q, k_new, v_new, pos, rope, q_out, n_tokens)
+PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return plain([&]() -> int {
+    if (n != 9) return -1;
+    Reader r(g_rope_append != nullptr, a[0], a[1]);
+    if (!r.ok) return -1;
+    const Rows w(r, a[3], a[4], true);
+    const int32_t *pos = lengths(r, a[5]), *counts = lengths_or_none(r, a[8]);
+    kvq_rope rope;
+    if (!r.ok || !r.need(copy_struct(a[6], g_rope_class, g_cache_attr, &rope))) return -1;
+    const auto k = THPVariable_Unpack(a[3]).sizes();
+    if (!r.need(k[0] == r.layout.batch && k[1] == r.layout.kv_heads && k[3] == r.layout.head_dim)) return -1;
+    const void* q = nullptr;
+    void* q_out = nullptr;
+    int64_t sb = 0, st = 0, sh = 0, heads = 0;
+    if (a[2] != Py_None) {
+      const at::Tensor *qt = r.tensor(a[2]), *ot = r.tensor(a[7]);
+      if (!r.ok || !r.need(qt->dim() == 4 && qt->size(0) == k[0] && qt->size(1) == k[2] && qt->size(3) == k[3] && qt->stride(3) == 1)) return -1;
+      if (!r.need(r.dtype(*qt) == w.type && ot->scalar_type() == qt->scalar_type() && ot->sizes() == qt->sizes() && ot->is_contiguous())) return -1;
+      heads = qt->size(2);
+      if (!r.need(heads <= INT32_MAX)) return -1;
+      q = qt->data_ptr(); q_out = ot->data_ptr();
+      sb = qt->stride(0); st = qt->stride(1); sh = qt->stride(2);
+    } else if (!r.need(a[7] == Py_None)) {
+      return -1;
+    }
+    return released([&] {
+      return g_rope_append(&r.layout, &r.cache, q, sb, st, sh, (int32_t)heads, q_out, w.k, w.v, w.type, w.sb, w.sh, w.st, pos, counts, (int32_t)w.n, &rope,
+                           r.stream);
+    });
+  });
+}
+
+// (layout, cache, q, q_lens, seq_lens, max_seq_len, window, sinks, softmax_scale, out, workspace)
+PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return plain([&]() -> int {
+    if (n != 11) return -1;
+    Reader r(g_chunk != nullptr, a[0], a[1]);
+    if (!r.ok) return -1;
+    const at::Tensor *q = r.tensor(a[2]), *out = r.tensor(a[9]), *ws = a[10] == Py_None ? nullptr : r.tensor(a[10]);
+    const int32_t *q_lens = lengths_or_none(r, a[3]), *seq_lens = lengths_or_none(r, a[4]);
+    const int32_t bound = r.int32(a[5]), window = r.int32(a[6]), sinks = r.int32(a[7]);
+    const float scale = r.real(a[8]);
+    if (!r.ok || !r.need(q->dim() == 4 && q->size(0) == r.layout.batch && q->size(3) == r.layout.head_dim && q->stride(3) == 1)) return -1;
+    if (!r.need(out->is_contiguous() && out->sizes() == q->sizes() && q->size(1) <= INT32_MAX && q->size(2) <= INT32_MAX)) return -1;
+    const kvq_dtype q_type = r.dtype(*q), out_type = r.dtype(*out);
+    if (!r.ok) return -1;
+    const void* const qp = q->data_ptr();
+    void *const op = out->data_ptr(), *const wp = ws ? ws->data_ptr() : nullptr;
+    const int64_t sb = q->stride(0), st = q->stride(1), sh = q->stride(2);
+    const int32_t heads = (int32_t)q->size(2), n_q = (int32_t)q->size(1);
+    const size_t bytes = ws ? ws->nbytes() : 0;
+    return released([&] {
+      return g_chunk(&r.layout, &r.cache, qp, q_type, heads, sb, st, sh, n_q, q_lens, seq_lens, bound, window, sinks, scale, op, out_type, wp, bytes, r.stream);
+    });
+  });
+}
+
+// (layout, cache, q, seq_lens, max_seq_len, window, sinks, softmax_scale, out, workspace)
+PyObject* window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return plain([&]() -> int {
+    if (n != 10) return -1;
+    Reader r(g_window != nullptr, a[0], a[1]);
+    if (!r.ok) return -1;
+    const Attention t(r, a[2], a[7], a[8], a[9]);
+    const int32_t* lens = lengths_or_none(r, a[3]);
+    const int32_t bound = r.int32(a[4]), window = r.int32(a[5]), sinks = r.int32(a[6]);
+    if (!r.ok) return -1;
+    const at::Tensor& q = THPVariable_Unpack(a[2]);
+    if (!r.need(q.size(0) == r.layout.batch && q.size(2) == r.layout.head_dim)) return -1;
+    return released([&] {
+      return g_window(&r.layout, &r.cache, t.q, t.q_type, t.heads, lens, bound, window, sinks, t.scale, t.out, t.out_type, t.ws, t.ws_bytes, r.stream);
+    });
+  });
+}
+
 // (five addresses, in the order of the pointers above: the entry points of the library that kvq.py has loaded; then its classes
 // Layout and Cache)
 PyObject* bind(PyObject*, PyObject* args) {
@@ -252,6 +335,17 @@ PyObject* bind(PyObject*, PyObject* args) {
   Py_INCREF(cache); Py_XSETREF(g_cache_class, cache);
   Py_RETURN_NONE;
 }
+// (three more: rope_append, chunk_attention, window_attention; then the class Rope)
+PyObject* bind_several(PyObject*, PyObject* args) {
+  unsigned long long p[3];
+  PyObject* rope;
+  if (!PyArg_ParseTuple(args, "KKKO", &p[0], &p[1], &p[2], &rope)) return nullptr;
+  g_rope_append = reinterpret_cast<decltype(g_rope_append)>(p[0]);
+  g_chunk = reinterpret_cast<decltype(g_chunk)>(p[1]);
+  g_window = reinterpret_cast<decltype(g_window)>(p[2]);
+  Py_INCREF(rope); Py_XSETREF(g_rope_class, rope);
+  Py_RETURN_NONE;
+}
 // torch's device runtime is up in this process (kvq.py says so after a call that went its own way).
 PyObject* ready(PyObject*, PyObject*) {
   g_pid = getpid();
@@ -260,7 +354,8 @@ PyObject* ready(PyObject*, PyObject*) {
 
 #define KVQ_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KVQ_FAST(quantize_append), KVQ_FAST(decode_attention), KVQ_FAST(decode_attention_varlen),
-                         KVQ_FAST(decode_step), KVQ_FAST(decode_step_varlen), {"bind", bind, METH_VARARGS, nullptr},
+                         KVQ_FAST(decode_step), KVQ_FAST(decode_step_varlen), KVQ_FAST(rope_append), KVQ_FAST(chunk_attention), KVQ_FAST(window_attention),
+                         {"bind", bind, METH_VARARGS, nullptr}, {"bind_several", bind_several, METH_VARARGS, nullptr},
                          {"ready", ready, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvq_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

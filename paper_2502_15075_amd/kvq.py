@@ -70,7 +70,7 @@ def _extension():
 
 def _bind(lib) -> None:
     """Hands the library's entry points to the extension module, if there is one."""
-    global _fast, _fast_append, _fast_attention, _fast_attention_varlen, _fast_step, _fast_step_varlen
+    global _fast, _fast_append, _fast_attention, _fast_attention_varlen, _fast_step, _fast_step_varlen, _fast_rope, _fast_chunk, _fast_window
     if _fast is None:
         _fast = _extension()
     if _fast is None:
@@ -79,6 +79,8 @@ def _bind(lib) -> None:
                                                          lib.kvq_decode_step, lib.kvq_decode_step_varlen)], Layout, Cache)
     _fast_append, _fast_attention, _fast_attention_varlen = _fast.quantize_append, _fast.decode_attention, _fast.decode_attention_varlen
     _fast_step, _fast_step_varlen = _fast.decode_step, _fast.decode_step_varlen
+    _fast.bind_several(*[C.cast(f, C.c_void_p).value for f in (lib.kvq_rope_append, lib.kvq_chunk_attention, lib.kvq_window_attention)], Rope)
+    _fast_rope, _fast_chunk, _fast_window = _fast.rope_append, _fast.chunk_attention, _fast.window_attention
 
 
 def _not_loaded(*args):
@@ -140,6 +142,7 @@ def load():
 
 
 _fast_append = _fast_attention = _fast_attention_varlen = _fast_step = _fast_step_varlen = _not_loaded
+_fast_rope = _fast_chunk = _fast_window = _not_loaded
 
 
 def status_string(status: int) -> str:
@@ -192,7 +195,7 @@ def _check(status: int, where: str) -> None:
 
 
 # What a call costs here is object building: attribute reads of tensors (0.1 to 0.3 us each) and ctypes temporaries (0.1 us
-# each).  The five calls of a decode loop therefore go to the extension module first; what it leaves comes by the statements
+# each).  The calls of a decode loop therefore go to the extension module first; what it leaves comes by the statements
 # below, where numbers are passed as numbers (the declared argument types convert them) and a tensor attribute is read once.
 
 def _stream_ptr() -> int:
@@ -442,6 +445,13 @@ def rope_append(layout: Layout, cache: Cache, q, k_new: torch.Tensor, v_new: tor
     tensor [B]; n_tokens, likewise, where sequences bring fewer than n), keys rotated by their positions' angles.  q: [B, n, H_q, D] of
     the same type (last axis contiguous), rotated into q_out (contiguous, of q's shape; q itself where q is contiguous; made here when it
     is None), or None.  Returns q_out."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    st = _fast_rope(layout, cache, q, k_new, v_new, pos, rope, q_out, n_tokens)
+    if st is not None:
+        if st:
+            _check(st, "kvq_rope_append")
+        return q_out
     shape, strides, dtype = k_new.shape, k_new.stride(), k_new.dtype
     assert shape == v_new.shape and dtype == v_new.dtype and len(shape) == 4 and shape[:2] == (layout.batch, layout.kv_heads)
     assert shape[3] == layout.head_dim and strides == v_new.stride() and strides[3] == 1
@@ -450,8 +460,6 @@ def rope_append(layout: Layout, cache: Cache, q, k_new: torch.Tensor, v_new: tor
     if q is not None:
         heads, qs = q.size(2), q.stride()
         assert q.dim() == 4 and q.shape == (shape[0], shape[2], heads, shape[3]) and q.dtype == dtype and qs[3] == 1
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
         assert q_out.shape == q.shape and q_out.dtype == dtype and q_out.is_contiguous()
     else:
         assert q_out is None
@@ -473,6 +481,11 @@ def chunk_attention(layout: Layout, cache: Cache, q: torch.Tensor, q_lens, seq_l
     """Causal attention of the last tokens of every sequence over its cache.  q: [B, n_q, H_q, D] fp16/bf16, last axis contiguous; out:
     contiguous fp32/fp16/bf16 of q's shape; q_lens, seq_lens: int32 device tensors [B] (None: n_q and max_seq_len for all); window: newest
     tokens a query sees, its own among them (0: all); sinks: first tokens it sees besides; workspace: uint8 device tensor or None."""
+    st = _fast_chunk(layout, cache, q, q_lens, seq_lens, max_seq_len, window, sinks, softmax_scale, out, workspace)
+    if st is not None:
+        if st:
+            _check(st, "kvq_chunk_attention")
+        return out
     shape, strides = q.shape, q.stride()
     assert len(shape) == 4 and shape[0] == layout.batch and shape[3] == layout.head_dim and strides[3] == 1
     assert out.is_contiguous() and out.shape == shape and _lens_ok(q_lens, layout) and _lens_ok(seq_lens, layout)
@@ -493,6 +506,11 @@ def window_attention(layout: Layout, cache: Cache, q: torch.Tensor, seq_lens, ma
                      softmax_scale: float, out: torch.Tensor, workspace) -> torch.Tensor:
     """decode_attention_varlen with a sliding window and sinks: the query of sequence b (position seq_lens[b] - 1) sees its newest
     `window` tokens (0: all) and the first `sinks`.  q, out: [B, H_q, D] contiguous; seq_lens: int32 device tensor [B] or None."""
+    st = _fast_window(layout, cache, q, seq_lens, max_seq_len, window, sinks, softmax_scale, out, workspace)
+    if st is not None:
+        if st:
+            _check(st, "kvq_window_attention")
+        return out
     shape = q.shape
     assert q.is_contiguous() and out.is_contiguous() and len(shape) == 3 and out.shape == shape and _lens_ok(seq_lens, layout)
     assert shape[0] == layout.batch and shape[2] == layout.head_dim
