@@ -16,8 +16,9 @@
 // summed.  Key scales are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the
 // query's group sums, each split into two binary16 parts.
 //
-// Bound by instruction issue and by power: of a wavefront's tile (34 matrix instructions of 32 cycles) the vector instructions, unpacking's share
-// included, take about 1300 cycles beside 1088; matrix instructions of ordinary operands alone run at 20 ns each under sustained load, 14 with zeros.
+// Bound by LDS, by issue and by power together: of 2.97 million cycles of the call below the LDS reads take 1.8 (50 of 16 bytes a lane and wavefront
+// tile, 8 cycles each; a third of them are scales), vector instructions 1.4, matrix instructions 1.1; matrix instructions of ordinary operands alone run at
+// 20 ns each under sustained load, 14 with zeros.  Unpacking before the products in half of a workgroup's wavefronts, or priorities, changed nothing.
 // 2048 query tokens of 32 heads on 32768 tokens, 4/2 bits: 1.06 TFLOP in 1253 us (850 TFLOP/s; a product of 8192^3 reaches 1313).  What each
 // step gave there: 128 rows a workgroup, two of them a compute unit, each tile loaded when its turn came 1640; the next tile's words on
 // their way meanwhile 1577; 256 rows, so that unpacking is shared by eight wavefronts 1419; subnormal codes, uniform addresses and a maximum
