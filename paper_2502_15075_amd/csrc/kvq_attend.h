@@ -42,13 +42,6 @@ __device__ __forceinline__ uint32_t raw_to_half2(uint32_t x, bool bf) {
   return as_u32(h);
 }
 
-// Where the lowest bit k of a code lies in its binary16 lane.  2^(-14 - k) of a code's step is lost: for binary32 outputs (FINE) the codes go as high
-// as they fit, which leaves 2^-24 of a group's range whatever the width; otherwise where they need fewest shifts.
-template <int B, bool FINE> constexpr int code_base() { return FINE ? 10 - B : B == 1 || B == 2 ? 6 : B == 3 || B == 4 || B == 6 ? 4 : 0; }
-template <int B, bool FINE> constexpr float code_unit() { return B == 16 ? 1.0f : 1.0f / (float)(1 << (24 - code_base<B == 16 ? 8 : B, FINE>())); }
-// x >> n, n < 0: x << -n
-template <int N> __device__ __forceinline__ uint32_t shifted(uint32_t x) { return N >= 0 ? x >> (N >= 0 ? N : 0) : x << (N < 0 ? -N : 0); }
-
 // Channel order inside a 32-channel chunk of an unpacked key row: with P = 16 / (field width), field pair (p, p + P) of dword w is
 // slots 2 (w P + p) and + 1.  The slot of channel x (0..31):
 __device__ __forceinline__ int key_slot(int x, int per) {

@@ -10,20 +10,21 @@
 // wants them.  Tokens reach the matrix rows with bits 3 and 4 of their number swapped, which makes the packed value blocks' order the
 // operand's order.
 //
-// A tile of 64 tokens is unpacked once per workgroup into LDS: keys as codes (binary16 subnormals, a whole number times a
-// power of two that the scale takes back), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are
-// rounded alike).  For outputs in binary32 (FINE) weights and values travel as two binary16 parts each, 2^-22 of them, and three products are
-// summed.  Key scales are applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the
-// query's group sums, each split into two binary16 parts.
+// A tile of 64 tokens is unpacked once per workgroup into LDS: keys as binary16 codes (0 .. 255: exact, so their products with the query
+// are too), values as binary16 reconstructions (rounded once, half a unit of 2^-11; the weights are rounded alike).  For outputs in
+// binary32 (FINE) weights and values travel as two binary16 parts each, 2^-22 of them, and three products are summed.  Key scales are
+// applied to the binary32 sums of their group, key zeros come in through one more matrix instruction against the query's group sums,
+// each split into two binary16 parts.
 //
-// Bound by LDS, by issue and by power together: of 2.97 million cycles of the call below the LDS reads take 1.8 (50 of 16 bytes a lane and wavefront
-// tile, 8 cycles each; a third of them are scales), vector instructions 1.4, matrix instructions 1.1; matrix instructions of ordinary operands alone run at
-// 20 ns each under sustained load, 14 with zeros.  Unpacking before the products in half of a workgroup's wavefronts, or priorities, changed nothing.
-// 2048 query tokens of 32 heads on 32768 tokens, 4/2 bits: 1.06 TFLOP in 1253 us (850 TFLOP/s; a product of 8192^3 reaches 1313).  What each
-// step gave there: 128 rows a workgroup, two of them a compute unit, each tile loaded when its turn came 1640; the next tile's words on
-// their way meanwhile 1577; 256 rows, so that unpacking is shared by eight wavefronts 1419; subnormal codes, uniform addresses and a maximum
-// that is looked for only when a sum shows that it lags 1380 on one card, 1253 to 1285 on others.  Steps of four matrix instructions with the next
-// operands read ahead and the last scores' arithmetic between them, in one wavefront's code, took 30 % more vector instructions and 1685 us.
+// Bound by LDS, by issue and by power together.  2048 query tokens of 32 heads on 32768 tokens, 4/2 bits: 1.06 TFLOP in 1226 us (869 TFLOP/s; a
+// product of 8192^3 reaches 1313).  Of its 2.9 million cycles a compute unit's LDS reads take about 1.5 (42 of 16 bytes a lane and wavefront tile, 8
+// cycles each), a SIMD's vector instructions 1.4, its matrix instructions 1.1; matrix instructions of ordinary operands alone run at 20 ns
+// each under sustained load, 14 with zeros.  What the steps gave: 128 rows a workgroup, two of them a compute unit, each tile loaded when
+// its turn came 1640; the next tile's words on their way meanwhile 1577; 256 rows, so that unpacking is shared by eight wavefronts 1419;
+// uniform addresses and a maximum that is looked for only when a sum shows that it lags 1380 on that card, 1253 on this; key scales read as
+// binary16, all groups of four tokens at a time, 1226.  Nothing: unpacking before the products in half of a workgroup's wavefronts, priorities.
+// Steps of four matrix instructions with the next operands read ahead and the last scores' arithmetic between them, in one wavefront's code, took
+// 30 % more vector instructions and 1685 us.
 #include "kvq_attend.h"
 #include "kvq_few.h"
 
@@ -56,11 +57,10 @@ template <int B> __device__ __forceinline__ void load_key_chunk(uint32_t* w, con
     for (int i = 0; i < B; ++i) w[i] = p[i];
   }
 }
-// ... and its codes as 16 pairs of binary16 subnormals in slot order, four 16-byte pieces (PIECES 2: the first or the second half, B / 2 dwords).
-template <int B, bool FINE, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, u32x4 (&out)[PIECES]) {
+// ... and its codes as 16 binary16 pairs in slot order, four 16-byte pieces (PIECES 2: the first or the second half, B / 2 dwords).
+template <int B, int PIECES = 4> __device__ __forceinline__ void unpack_key_chunk(const uint32_t* w, bool raw_bf, uint32_t one_k, u32x4 (&out)[PIECES]) {
   constexpr int LO = code_lo_bits<B>(), HI = code_hi_bits<B>();
   constexpr int P = 16 / LO;                       // pairs per dword
-  constexpr int base = B == 16 ? 0 : code_base<B, FINE>();
   constexpr uint32_t mask = B == 16 ? 0xFFFFFFFFu : ((1u << LO) - 1u) * 0x00010001u;
 #pragma unroll
   for (int s = 0; s < 4 * PIECES; ++s) {
@@ -77,8 +77,7 @@ template <int B, bool FINE, int PIECES = 4> __device__ __forceinline__ void unpa
         x |= ((w[LO + at / 32] >> (at % 32)) & hmask) << LO;
         x |= ((w[LO + next / 32] >> (next % 32)) & hmask) << (LO + 16);
       }
-      if constexpr (HI != 0) out[s >> 2][s & 3] = x << base;
-      else out[s >> 2][s & 3] = (LO * f >= base ? w[dw] >> (LO * f - base) : w[dw] << (base - LO * f)) & (mask << base);
+      out[s >> 2][s & 3] = as_u32(whole_to_half2(x, HI != 0 ? ~0u : mask, one_k));
     }
   }
 }
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
   constexpr int kWaves = tile_waves(BK), kTileRows = kRowsPerWave * kWaves;
   constexpr int kTileBytes = kTileTokens * kHeadDim * 2, kBuffers = kAhead ? 2 : 1, kBufferBytes = (FINE ? 3 : 2) * kTileBytes;
   __shared__ __attribute__((aligned(16))) uint8_t sm_tile[kBuffers * kBufferBytes];            // keys, values, the values' second parts
-  __shared__ __attribute__((aligned(16))) float sm_scale_[kBuffers][4][kTileTokens];           // key scales, by matrix row
+  __shared__ __attribute__((aligned(16))) uint16_t sm_scale_[kBuffers][kTileTokens * NG];       // key scales, by matrix row
   __shared__ __attribute__((aligned(16))) uint32_t sm_zero_[kBuffers][kTileTokens][4];         // key zeros, each twice
   __shared__ __attribute__((aligned(16))) uint32_t sm_qsum[kTileRows][4];                      // group sums of the query, two parts each
   __shared__ float sm_kappa[kTileRows];
@@ -205,19 +204,6 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
   float m = kNoMax, l = 0.0f;
   const bool two_parts = g.bits_v != 16;                   // (patterns of an unquantized plane have no second part)
-  // key codes stand as binary16 subnormals; this takes them back to whole numbers
-  auto unit_of = [&]() -> float {
-    switch (kAhead ? BK : g.bits_k) {
-      case 1: return 1.0f / code_unit<1, FINE>();
-      case 2: return 1.0f / code_unit<2, FINE>();
-      case 3: return 1.0f / code_unit<3, FINE>();
-      case 4: return 1.0f / code_unit<4, FINE>();
-      case 6: return 1.0f / code_unit<6, FINE>();
-      case 8: return 1.0f / code_unit<8, FINE>();
-    }
-    return 1.0f;
-  };
-  const float from_codes = unit_of();
   const uint32_t one_k = one_k_pattern(), v_mask = ((1u << min(g.bits_v, 15)) - 1u) * 0x00010001u;
 
   // (a block of tiles: [0, sink_tiles) and [first, ...))
@@ -256,7 +242,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     for (int i = 0; i < kPieces; ++i)
       *reinterpret_cast<u32x4*>(sm_k + k_row * 256 + (((4 * chunk + kPieces * sub + i) ^ (k_row & 15)) << 4)) = piece[i];
     if (!seen_by_some(t0 + tok) || chunk >= NG) km = 0;
-    sm_scale_[at][chunk][k_row] = widen16((uint16_t)km, false) * from_codes;
+    if (chunk < NG) sm_scale_[at][k_row * NG + chunk] = (uint16_t)km;
     sm_zero_[at][k_row][chunk] = (km >> 16) * 0x00010001u;
 
     const int tv = t0 + 32 * vblk + 4 * j;                 // the lane's tokens: tv + 16 x4 + r
@@ -326,6 +312,10 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
 #pragma unroll
         for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
         s = mma32(*reinterpret_cast<const u32x4*>(sm_zero_[at][32 * blk + col]), qs, zero);
+        typedef _Float16 scales4 __attribute__((ext_vector_type(4 * NG)));
+        scales4 sc[4];                                     // 4 tokens, NG groups each
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sc[q] = *reinterpret_cast<const scales4*>(&sm_scale_[at][(32 * blk + 8 * q + 4 * hh) * NG]);
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
           float16v part = zero;
@@ -333,11 +323,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
           for (int kk = n * (8 / NG); kk < (n + 1) * (8 / NG); ++kk)
             part = mma32(*reinterpret_cast<const u32x4*>(kt + col * 256 + (((2 * kk + hh) ^ (col & 15)) << 4)), qb[kk], part);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float4v sc = *reinterpret_cast<const float4v*>(&sm_scale_[at][n][32 * blk + 8 * q + 4 * hh]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(sc[e], part[4 * q + e], s[4 * q + e]);
-          }
+          for (int i = 0; i < 16; ++i) s[i] = fmaf((float)sc[i >> 2][(i & 3) * NG + n], part[i], s[i]);
         }
       }
       // register i: token 16 (i / 4 % 2) + 8 (i / 8) + 4 hh + i % 4 of the block
@@ -422,7 +408,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     auto unpack = [&](int ti, int at) {
       u32x4 piece[kPieces];
       uint32_t f[kPairs];
-      unpack_key_chunk<BK, FINE, kPieces>(raw_k, raw_bf, piece);
+      unpack_key_chunk<BK, kPieces>(raw_k, raw_bf, one_k, piece);
       value_fields<BV, false, kPairs>(raw_v, f);
       store(piece, raw_km, f, raw_vm, false, first_token(ti), at);
     };
@@ -454,13 +440,13 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
       u32x4 piece[4], vm[4];
       uint32_t w[16], f[16], km;
       switch (bits_k) {
-        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1, FINE>(w, raw_bf, piece); break;
-        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2, FINE>(w, raw_bf, piece); break;
-        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3, FINE>(w, raw_bf, piece); break;
-        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4, FINE>(w, raw_bf, piece); break;
-        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6, FINE>(w, raw_bf, piece); break;
-        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8, FINE>(w, raw_bf, piece); break;
-        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16, FINE>(w, raw_bf, piece); break;
+        case 1: load_key_chunk<1>(w, kp); unpack_key_chunk<1>(w, raw_bf, one_k, piece); break;
+        case 2: load_key_chunk<2>(w, kp); unpack_key_chunk<2>(w, raw_bf, one_k, piece); break;
+        case 3: load_key_chunk<3>(w, kp); unpack_key_chunk<3>(w, raw_bf, one_k, piece); break;
+        case 4: load_key_chunk<4>(w, kp); unpack_key_chunk<4>(w, raw_bf, one_k, piece); break;
+        case 6: load_key_chunk<6>(w, kp); unpack_key_chunk<6>(w, raw_bf, one_k, piece); break;
+        case 8: load_key_chunk<8>(w, kp); unpack_key_chunk<8>(w, raw_bf, one_k, piece); break;
+        default: load_key_chunk<16>(w, kp); unpack_key_chunk<16>(w, raw_bf, one_k, piece); break;
       }
       switch (bits_v) {
         case 1: load_value_half<1>(w, vp, lane, half); value_fields<1>(w, f); break;

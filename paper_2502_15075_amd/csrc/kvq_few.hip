@@ -55,6 +55,12 @@ __device__ __forceinline__ float meta_z(uint32_t m) { return (float)as_half2(m)[
 template <int B> constexpr bool key_swizzled() { return (B & (B - 1)) == 0 && B > 1; }
 template <int B> __device__ __forceinline__ int key_swizzle(int row) { return key_swizzled<B>() ? (row * B / 16) & (B - 1) : 0; }
 
+// Where the lowest bit k of a code lies in its binary16 lane.  2^(-14 - k) of a code's step is lost: for binary32 outputs (FINE) the codes go as high
+// as they fit, which leaves 2^-24 of a group's range whatever the width; otherwise where they need fewest shifts.
+template <int B, bool FINE> constexpr int code_base() { return FINE ? 10 - B : B == 1 || B == 2 ? 6 : B == 3 || B == 4 || B == 6 ? 4 : 0; }
+template <int B, bool FINE> constexpr float code_unit() { return B == 16 ? 1.0f : 1.0f / (float)(1 << (24 - code_base<B == 16 ? 8 : B, FINE>())); }
+// x >> n, n < 0: x << -n
+template <int N> __device__ __forceinline__ uint32_t shifted(uint32_t x) { return N >= 0 ? x >> (N >= 0 ? N : 0) : x << (N < 0 ? -N : 0); }
 // Fields of W bits at bits AT and 16 + AT of x, their lowest bits taken to BASE and 16 + BASE
 template <int W, int AT, int BASE> __device__ __forceinline__ uint32_t field(uint32_t x) {
   return shifted<AT - BASE>(x) & (((1u << W) - 1u) * 0x00010001u << BASE);
