@@ -22,7 +22,7 @@
 // each under sustained load, 14 with zeros.  What the steps gave: 128 rows a workgroup, two of them a compute unit, each tile loaded when
 // its turn came 1640; the next tile's words on their way meanwhile 1577; 256 rows, so that unpacking is shared by eight wavefronts 1419;
 // uniform addresses and a maximum that is looked for only when a sum shows that it lags 1380 on that card, 1253 on this; key scales read as
-// binary16, all groups of four tokens at a time, 1226.  Nothing: unpacking before the products in half of a workgroup's wavefronts, priorities.
+// binary16, two groups of four tokens at a time, 1226.  Nothing: unpacking before the products in half of a workgroup's wavefronts, priorities.
 // Steps of four matrix instructions with the next operands read ahead and the last scores' arithmetic between them, in one wavefront's code, took
 // 30 % more vector instructions and 1685 us.
 #include "kvq_attend.h"
@@ -156,9 +156,10 @@ template <int BK, int BV, int NG, bool FINE>
 __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const ChunkArgs a) {
   constexpr bool kAhead = BK != 0;
   constexpr int kWaves = tile_waves(BK), kTileRows = kRowsPerWave * kWaves;
+  constexpr int kPair = NG < 2 ? 1 : 2;
   constexpr int kTileBytes = kTileTokens * kHeadDim * 2, kBuffers = kAhead ? 2 : 1, kBufferBytes = (FINE ? 3 : 2) * kTileBytes;
   __shared__ __attribute__((aligned(16))) uint8_t sm_tile[kBuffers * kBufferBytes];            // keys, values, the values' second parts
-  __shared__ __attribute__((aligned(16))) uint16_t sm_scale_[kBuffers][kTileTokens * NG];       // key scales, by matrix row
+  __shared__ __attribute__((aligned(16))) uint16_t sm_scale_[kBuffers][NG / kPair][kTileTokens * kPair];       // key scales, by matrix row, two groups side by side
   __shared__ __attribute__((aligned(16))) uint32_t sm_zero_[kBuffers][kTileTokens][4];         // key zeros, each twice
   __shared__ __attribute__((aligned(16))) uint32_t sm_qsum[kTileRows][4];                      // group sums of the query, two parts each
   __shared__ float sm_kappa[kTileRows];
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
     for (int i = 0; i < kPieces; ++i)
       *reinterpret_cast<u32x4*>(sm_k + k_row * 256 + (((4 * chunk + kPieces * sub + i) ^ (k_row & 15)) << 4)) = piece[i];
     if (!seen_by_some(t0 + tok) || chunk >= NG) km = 0;
-    if (chunk < NG) sm_scale_[at][k_row * NG + chunk] = (uint16_t)km;
+    if (chunk < NG) sm_scale_[at][chunk / kPair][k_row * kPair + chunk % kPair] = (uint16_t)km;
     sm_zero_[at][k_row][chunk] = (km >> 16) * 0x00010001u;
 
     const int tv = t0 + 32 * vblk + 4 * j;                 // the lane's tokens: tv + 16 x4 + r
@@ -312,18 +313,20 @@ __global__ __launch_bounds__(64 * tile_waves(BK), 2) void chunk_kernel(const Chu
 #pragma unroll
         for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
         s = mma32(*reinterpret_cast<const u32x4*>(sm_zero_[at][32 * blk + col]), qs, zero);
-        typedef _Float16 scales4 __attribute__((ext_vector_type(4 * NG)));
-        scales4 sc[4];                                     // 4 tokens, NG groups each
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sc[q] = *reinterpret_cast<const scales4*>(&sm_scale_[at][(32 * blk + 8 * q + 4 * hh) * NG]);
+        typedef _Float16 scales4 __attribute__((ext_vector_type(4 * kPair)));
+        scales4 sc[4];                                     // of 4 tokens each, two groups
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
+          if (n % kPair == 0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sc[q] = *reinterpret_cast<const scales4*>(&sm_scale_[at][n / kPair][(32 * blk + 8 * q + 4 * hh) * kPair]);
+          }
           float16v part = zero;
 #pragma unroll
           for (int kk = n * (8 / NG); kk < (n + 1) * (8 / NG); ++kk)
             part = mma32(*reinterpret_cast<const u32x4*>(kt + col * 256 + (((2 * kk + hh) ^ (col & 15)) << 4)), qb[kk], part);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = fmaf((float)sc[i >> 2][(i & 3) * NG + n], part[i], s[i]);
+          for (int i = 0; i < 16; ++i) s[i] = fmaf((float)sc[i >> 2][(i & 3) * kPair + n % kPair], part[i], s[i]);
         }
       }
       // register i: token 16 (i / 4 % 2) + 8 (i / 8) + 4 hh + i % 4 of the block
